@@ -38,7 +38,7 @@ typedef enum {
     LUVC_OK = 0,
     LUVC_ERR_INVALID_ARG = 1,  /* NULL pointer, non-positive size, inconsistent schedule ...   */
     LUVC_ERR_UNSUPPORTED = 2,  /* valid request outside what the kernels implement              */
-    LUVC_ERR_WORKSPACE = 3,    /* workspace missing, misaligned or smaller than the query says  */
+    LUVC_ERR_WORKSPACE = 3,    /* workspace missing, misaligned or smaller than the query says; too few free pages */
     LUVC_ERR_HIP = 4           /* a HIP launch failed; luvc_last_error() carries hipGetErrorString */
 } luvc_status;
 
@@ -323,6 +323,116 @@ luvc_status luvc_spu_stage_ragged(const void* x, int n_samples, const int32_t* N
                                   luvc_dtype dtype, const int32_t* sigma, int use_hamming, const int32_t* n_keep,
                                   const int32_t* origin_in, float* scores, int32_t* kept_idx, int32_t* origin_out,
                                   void* x_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Paged key-value cache: where the tokens that OIM and SPU leave over live while the language model writes its answer.
+ * A pool holds pages of page_tokens tokens for every layer; a sequence is a row of a table with the numbers of its pages,
+ * so that its token at position p lies in row p % page_tokens of page table[p / page_tokens] - the same page number in
+ * every layer that shares the table (the layers between two SPU stages do; another group of layers has a table of its own).
+ *
+ *   k, v         device dtype: head h of row r of page p in layer l starts at
+ *                l * layer_stride + ((p * n_heads + h) * page_tokens + r) * D
+ *   sizes        device [n_pages, page_tokens] int32, or NULL: how many tokens were merged into the one that is cached
+ *                there (the size vector of Algorithm 1), for all layers.  A token whose size is below 1 takes no part in
+ *                attention: pruned in place, or the padding of a batch
+ *   layer_stride elements, >= n_pages * n_heads * page_tokens * D
+ *   page_tokens  a power of two from 16 to 1024
+ *   D            channels per head, 1..256
+ * Tables are device arrays [n_seqs, max_pages] int32.  An entry outside 0..n_pages-1 is no page (-1 behind the last page of
+ * a sequence, say): nothing is read or written there.
+ * The fields are read during a call only.  Calls that change the same pages are ordered by the caller, as are changes of
+ * tables and lengths against the calls that read them.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    int32_t* sizes;
+    int64_t layer_stride;
+    int32_t n_layers, n_pages, n_heads, page_tokens, D;
+    luvc_dtype dtype;
+} luvc_kv_cache;
+
+/*
+ * Puts the keys and values of new tokens in their places: tokens of a prompt, or one of every sequence.
+ *   layer       0..n_layers-1
+ *   k, v        device: head h of token t is [D] dtype at k + t * k_stride + h * D (and v, v_stride); strides in elements,
+ *               >= n_heads * D, so that both may be parts of one projection's output
+ *   sizes       device [tokens] int32: goes to the cache's sizes; NULL: 1 for every token where the cache has sizes
+ *   seq         device [tokens] int32: the table row a token belongs to, or NULL: token t is of row t.  A token whose row is
+ *               not in 0..n_seqs-1 (padding: -1) is left out
+ *   pos         device [tokens] int32: its position in the sequence; without a page at that position it is left out
+ * Two tokens with the same place: it holds parts of either afterwards.  tokens = 0 enqueues nothing.
+ * Limits: fewer than 2^25 tokens per call; every call on a cache: at most 1024 heads.
+ */
+luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                          const int32_t* sizes, int64_t tokens, const int32_t* seq, const int32_t* pos,
+                          const int32_t* table, int n_seqs, int max_pages, void* hip_stream);
+
+/*
+ * Attention of one new token per sequence over the cache (Eq. 3 with a single query row per head):
+ *   out[s,h] = sum_j a_j (v_j + log s_j),  a = softmax_j(scale * <q[s,h], k_j>)
+ * over the positions j < lengths[s] that have a page and (where the cache has sizes) a size of at least 1; query head h
+ * reads head h / (n_q_heads / n_heads) of the cache.  A sequence without such a position gets zeros.
+ *   q, out      device [n_seqs, n_q_heads, D] dtype with the sequences q_stride / out_stride elements apart (>= n_q_heads * D);
+ *               n_q_heads is a multiple of the cache's n_heads
+ *   lengths     device [n_seqs] int32; read as min(length, max_tokens, max_pages * page_tokens)
+ *   max_tokens  host, >= 1: no sequence is longer; the work is laid out for it, and the workspace
+ *   scale       host, or NULL: 1 / sqrt(D)
+ *   enhance     0: the plain values v_j; else the term log s_j as well (needs a cache with sizes)
+ * Logits, softmax and sums are fp32; with bf16 the weights a_j enter the product with the values in two bf16 terms (16 bits)
+ * and the output is rounded once.  The parts of a long sequence are joined in a fixed order: same input, same bits.
+ * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype); any contents, one per call
+ * in flight, also for calls in captured graphs.
+ * Limits: n_seqs * n_q_heads < 2^24.
+ */
+size_t luvc_kv_attend_workspace_bytes(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens);
+luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q, int64_t q_stride, int n_q_heads, int n_seqs,
+                           const int32_t* table, int max_pages, const int32_t* lengths, int max_tokens,
+                           const double* scale, int enhance, void* out, int64_t out_stride,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Applies a stage of SPU to the layers below it, which hold all tokens that the stage saw: of every sequence the tokens in
+ * front of the visual ones stay, of the visual ones those that the stage kept, then what follows them; the survivors close
+ * up, in all layers (and in the sizes).  Sequence i has lengths[i] tokens, the visual ones from position first[i] on.
+ *   lengths, first, span, n_keep   host [n_seqs]: 0 <= n_keep <= span, first + span <= lengths
+ *   kept_idx    device int32: n_keep[i] positions among the visual tokens, ascending, sequence after sequence - what
+ *               luvc_spu_stage and luvc_spu_stage_ragged return.  One outside 0..span[i]-1 moves nothing
+ *   table_in    device [n_seqs, max_pages_in]: where the tokens are
+ *   table_out   device [n_seqs, max_pages_out]: where they go; lengths[i] - span[i] + n_keep[i] tokens
+ * Pages of table_out must not be read by the call (from any of its sequences), with one exception: a page of tokens that stay
+ * where they are, so that first[i] / page_tokens pages of either table's row may be the same.
+ * The host arrays are used up when the call returns.  A call of more than 64 sequences is several launches.
+ * Limits: sequences of fewer than 2^29 tokens.
+ */
+luvc_status luvc_kv_compact(const luvc_kv_cache* cache, int n_seqs, const int32_t* lengths, const int32_t* first, const int32_t* span,
+                            const int32_t* n_keep, const int32_t* kept_idx, const int32_t* table_in, int max_pages_in,
+                            const int32_t* table_out, int max_pages_out, void* hip_stream);
+
+/*
+ * Copies pages src[i] to pages dst[i] in all layers, and their sizes.
+ *   src, dst    host [n]: page numbers; those of dst differ from each other and from all of src.  Used up when the call returns
+ * n = 0 enqueues nothing.
+ */
+luvc_status luvc_kv_copy_pages(const luvc_kv_cache* cache, const int32_t* src, const int32_t* dst, int n, void* hip_stream);
+
+/*
+ * Which pages are in use is the caller's host array refs [n_pages]: how many sequences hold each, 0 = free.
+ * luvc_kv_take    the n free pages with the lowest numbers, which then count 1
+ * luvc_kv_fork    n_children further sequences that go on from the `length` tokens in pages[0 .. ceil(length / page_tokens)-1]:
+ *                 full pages are shared (and count n_children more); of a partial last page every child gets a copy of the
+ *                 rows in use, in all layers, in a page taken for it (the lowest free ones, child after child), so that no
+ *                 sequence appends to a page that another reads
+ *                 child_pages   host [n_children, ceil(length / page_tokens)], written
+ * luvc_kv_release the n pages count one less (a page may be listed more than once)
+ * A release counts at once: a page that is free again may be written by what is enqueued next on the stream that last used
+ * it.  LUVC_ERR_WORKSPACE: fewer free pages than needed.  A call that fails leaves refs as they were.  luvc_kv_take and
+ * luvc_kv_release are host arithmetic only.
+ */
+luvc_status luvc_kv_take(int32_t* refs, int n_pages, int n, int32_t* pages);
+luvc_status luvc_kv_fork(const luvc_kv_cache* cache, int32_t* refs, const int32_t* pages, int64_t length, int n_children,
+                         int32_t* child_pages, void* hip_stream);
+luvc_status luvc_kv_release(int32_t* refs, int n_pages, const int32_t* pages, int n);
 
 /*
  * Timing aid for benchmarks (not a step of the paper's method; for callers that want the duration of

@@ -29,12 +29,20 @@ EXPORTS = ("luvc_version", "luvc_last_error", "luvc_oim_plan", "luvc_oim_workspa
            "luvc_spu_cascade_keeps", "luvc_spu_stage",
            "luvc_oim_plan_anyres", "luvc_oim_ragged_workspace_bytes", "luvc_oim_merge_ragged",
            "luvc_spu_ragged_workspace_bytes", "luvc_spu_stage_ragged",
+           "luvc_kv_write", "luvc_kv_attend_workspace_bytes", "luvc_kv_attend", "luvc_kv_compact", "luvc_kv_copy_pages",
+           "luvc_kv_take", "luvc_kv_fork", "luvc_kv_release",
            "luvc_profile_start", "luvc_profile_stop", "luvc_profile_kernel", "luvc_selftest_fdot2", "luvc_selftest_screen_tile",
            "luvc_selftest_screen_bound")
 
 
 class LuvcPass(ctypes.Structure):
     _fields_ = [("axis", ctypes.c_int32), ("m", ctypes.c_int32)]
+
+
+class LuvcKvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("sizes", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class LuvcError(RuntimeError):
@@ -100,6 +108,23 @@ def lib() -> ctypes.CDLL:
     L.luvc_spu_ragged_workspace_bytes.restype = sz
     L.luvc_spu_stage_ragged.argtypes = [vp, i, ip, i, i64, i, ip, i, ip, vp, vp, vp, vp, vp, vp, sz, vp]
     L.luvc_spu_stage_ragged.restype = i
+    cp = ctypes.POINTER(LuvcKvCache)
+    L.luvc_kv_write.argtypes = [cp, i, vp, i64, vp, i64, vp, i64, vp, vp, vp, i, i, vp]
+    L.luvc_kv_write.restype = i
+    L.luvc_kv_attend_workspace_bytes.argtypes = [cp, i, i, i]
+    L.luvc_kv_attend_workspace_bytes.restype = sz
+    L.luvc_kv_attend.argtypes = [cp, i, vp, i64, i, i, vp, i, vp, i, ctypes.POINTER(ctypes.c_double), i, vp, i64, vp, sz, vp]
+    L.luvc_kv_attend.restype = i
+    L.luvc_kv_compact.argtypes = [cp, i, ip, ip, ip, ip, vp, vp, i, vp, i, vp]
+    L.luvc_kv_compact.restype = i
+    L.luvc_kv_copy_pages.argtypes = [cp, ip, ip, i, vp]
+    L.luvc_kv_copy_pages.restype = i
+    L.luvc_kv_take.argtypes = [ip, i, i, ip]
+    L.luvc_kv_take.restype = i
+    L.luvc_kv_fork.argtypes = [cp, ip, ip, i64, i, ip, vp]
+    L.luvc_kv_fork.restype = i
+    L.luvc_kv_release.argtypes = [ip, i, ip, i]
+    L.luvc_kv_release.restype = i
     L.luvc_profile_start.argtypes = [ctypes.POINTER(vp), i]
     L.luvc_profile_start.restype = i
     L.luvc_profile_stop.argtypes = []
@@ -131,7 +156,8 @@ class _Native:
         self.i32, self.f32 = torch.int32, torch.float32
         self.raw_stream, self.device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         for name in ("luvc_oim_merge", "luvc_oim_merge_wide", "luvc_oim_merge_keyed", "luvc_value_enhance", "luvc_spu_score", "luvc_spu_score_static",
-                     "luvc_spu_prune", "luvc_spu_stage", "luvc_oim_merge_ragged", "luvc_spu_stage_ragged"):
+                     "luvc_spu_prune", "luvc_spu_stage", "luvc_oim_merge_ragged", "luvc_spu_stage_ragged",
+                     "luvc_kv_write", "luvc_kv_attend", "luvc_kv_compact", "luvc_kv_copy_pages", "luvc_kv_take", "luvc_kv_fork", "luvc_kv_release"):
             f = getattr(L, name)
             entry = ctypes.cast(f, ctypes.c_void_p).value
             if call is None:                            # host arrays are handed over as addresses here too
@@ -556,6 +582,152 @@ def luvc_spu_stage_ragged(x, lengths, sigmas, keeps=None, use_hamming: bool = Tr
     _check(nat.call(nat.luvc_spu_stage_ragged, x.data_ptr(), plan.n, N, D, x.stride(0), code, sigma, int(bool(use_hamming)), keep,
                     origin, scores.data_ptr(), ki, og, _ptr(xo) if K else None, workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
     return dict(scores=scores, kept_idx=kept_idx, origin=kept_origin, x=xo)
+
+
+class KvCache:
+    """A paged key-value cache on the caller's tensors: k, v CUDA [n_layers, n_pages, n_heads, page_tokens, D] (fp32 or bf16, a layer
+    contiguous), sizes int32 [n_pages, page_tokens] or None.  Holds the tensors and the structure the library reads."""
+
+    def __init__(self, k, v, sizes=None):
+        nat = _native()
+        assert k.is_cuda and k.dim() == 5 and v.shape == k.shape and v.dtype == k.dtype and v.device == k.device
+        assert k[0].is_contiguous() and v[0].is_contiguous() and (k.shape[0] == 1 or v.stride(0) == k.stride(0))
+        if sizes is not None:
+            assert sizes.device == k.device and sizes.dtype == nat.i32 and sizes.is_contiguous() and tuple(sizes.shape) == (k.shape[1], k.shape[3])
+        self.k, self.v, self.sizes = k, v, sizes
+        L, n_pages, n_heads, P, D = k.shape
+        stride = k.stride(0) if L > 1 else n_pages * n_heads * P * D
+        self.struct = LuvcKvCache(k.data_ptr(), v.data_ptr(), _ptr(sizes), stride, L, n_pages, n_heads, P, D, _dtype_code(k))
+        self.addr = ctypes.addressof(self.struct)
+        self.n_layers, self.n_pages, self.n_heads, self.page_tokens, self.D = L, n_pages, n_heads, P, D
+        self.dtype, self.device = k.dtype, k.device
+        self.index = k.get_device()
+
+
+def _here(nat, cache, *tensors):
+    """The library launches on the current GPU: its streams do not reach another one's memory."""
+    assert cache.index == nat.device(), "the cache is not on the current device"
+    for t in tensors:
+        assert t is None or t.get_device() == cache.index, "a tensor is not on the cache's device"
+
+
+def _host_ints(values):
+    """(what keeps them alive, address, count) of int32 on the host: a contiguous CPU tensor or array of them as it is, anything else copied."""
+    torch = _native().torch
+    if isinstance(values, torch.Tensor) and values.dtype == torch.int32 and not values.is_cuda and values.is_contiguous():
+        return values, values.data_ptr(), values.numel()
+    if isinstance(values, torch.Tensor):
+        values = values.flatten().tolist()
+    arr = _i32(list(values))
+    return arr, ctypes.addressof(arr), len(values)
+
+
+def luvc_kv_write(cache: KvCache, layer: int, k, v, pos, table, seq=None, sizes=None, stream=None):
+    """k, v [T, n_heads, D] (dense heads, tokens evenly strided) go to positions pos [T] of the table rows seq [T] (None: token t is of
+    row t); table int32 [n_seqs, max_pages]."""
+    nat = _native()
+    T, H, D = k.shape
+    assert v.shape == k.shape and (H, D) == (cache.n_heads, cache.D) and k.dtype == cache.dtype and v.dtype == cache.dtype
+    assert T == 0 or ((D == 1 or k.stride(2) == v.stride(2) == 1) and (H == 1 or k.stride(1) == v.stride(1) == D))
+    assert table.dim() == 2 and table.dtype == nat.i32 and table.is_contiguous()
+    _here(nat, cache, k, v, pos, table, seq, sizes)
+    for t in (pos, seq, sizes):
+        assert t is None or (t.dtype == nat.i32 and t.is_contiguous() and t.numel() == T)
+    ks, vs = (k.stride(0), v.stride(0)) if T > 1 else (H * D, H * D)
+    _check(nat.call(nat.luvc_kv_write, cache.addr, int(layer), k.data_ptr(), ks, v.data_ptr(), vs, _ptr(sizes), T, _ptr(seq), pos.data_ptr(),
+                    table.data_ptr(), table.shape[0], table.shape[1], nat.stream(stream)))
+
+
+def luvc_kv_attend_workspace_bytes(cache: KvCache, n_seqs: int, n_q_heads: int, max_tokens: int) -> int:
+    return lib().luvc_kv_attend_workspace_bytes(ctypes.byref(cache.struct), int(n_seqs), int(n_q_heads), int(max_tokens))
+
+
+def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Optional[int] = None, scale: Optional[float] = None,
+                   enhance: bool = False, workspace=None, stream=None, out=None):
+    """q [n_seqs, n_q_heads, D] (dense heads, sequences evenly strided): one new token per sequence attends to the lengths [n_seqs] int32
+    tokens in the pages of table [n_seqs, max_pages].  max_tokens: no sequence is longer (None: what the table holds).
+    Returns out [n_seqs, n_q_heads, D]."""
+    nat = _native()
+    S, Hq, D = q.shape
+    assert D == cache.D and q.dtype == cache.dtype and (S == 0 or ((D == 1 or q.stride(2) == 1) and (Hq == 1 or q.stride(1) == D)))
+    assert table.dim() == 2 and table.shape[0] == S and table.dtype == nat.i32 and table.is_contiguous()
+    assert lengths.dtype == nat.i32 and lengths.is_contiguous() and lengths.numel() == S
+    if max_tokens is None:
+        max_tokens = max(table.shape[1] * cache.page_tokens, 1)
+    if workspace is None:
+        need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
+        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
+    if out is None:
+        out = nat.torch.empty((S, Hq, D), dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and (S == 0 or ((D == 1 or out.stride(2) == 1) and (Hq == 1 or out.stride(1) == D)))
+    _here(nat, cache, q, table, lengths, workspace, out)
+    qs, os = (q.stride(0), out.stride(0)) if S > 1 else (Hq * D, Hq * D)
+    sc = None if scale is None else ctypes.c_double(scale)
+    _check(nat.call(nat.luvc_kv_attend, cache.addr, int(layer), q.data_ptr(), qs, Hq, S, table.data_ptr(), table.shape[1], lengths.data_ptr(),
+                    int(max_tokens), None if sc is None else ctypes.addressof(sc), int(bool(enhance)), out.data_ptr(), os,
+                    workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
+    return out
+
+
+def luvc_kv_compact(cache: KvCache, kept_idx, lengths, first, span, n_keep, table_in, table_out, stream=None) -> List[int]:
+    """Of sequence i with lengths[i] tokens (host integers, as first, span and n_keep) the span[i] visual ones from first[i] on shrink to the
+    n_keep[i] listed in kept_idx (CUDA int32, sequence after sequence).  Returns the lengths afterwards."""
+    nat = _native()
+    S = len(lengths)
+    assert len(first) == len(span) == len(n_keep) == S
+    for t in (table_in, table_out):
+        assert t.dim() == 2 and t.shape[0] == S and t.dtype == nat.i32 and t.is_contiguous()
+    _here(nat, cache, kept_idx, table_in, table_out)
+    arrays = [_host_ints(v) for v in (lengths, first, span, n_keep)]
+    after = [int(a) - int(b) + int(c) for a, b, c in zip(lengths, span, n_keep)]
+    assert kept_idx is None or (kept_idx.dtype == nat.i32 and kept_idx.is_contiguous() and kept_idx.numel() == sum(int(c) for c in n_keep))
+    _check(nat.call(nat.luvc_kv_compact, cache.addr, S, *(a[1] for a in arrays), _ptr(kept_idx), table_in.data_ptr(), table_in.shape[1],
+                    table_out.data_ptr(), table_out.shape[1], nat.stream(stream)))
+    return after
+
+
+def luvc_kv_copy_pages(cache: KvCache, src, dst, stream=None):
+    """Pages src[i] to pages dst[i] (host integers) in all layers."""
+    nat = _native()
+    _here(nat, cache)
+    (a, src_at, n), (b, dst_at, m) = _host_ints(src), _host_ints(dst)
+    assert n == m
+    _check(nat.call(nat.luvc_kv_copy_pages, cache.addr, src_at, dst_at, n, nat.stream(stream)))
+
+
+def _refs(refs):
+    torch = _native().torch
+    assert isinstance(refs, torch.Tensor) and refs.dtype == torch.int32 and not refs.is_cuda and refs.is_contiguous()
+    return refs.data_ptr()
+
+
+def luvc_kv_take(refs, n: int):
+    """The n lowest pages that refs (CPU int32 [n_pages], changed in place) counts 0; they count 1 then.  Returns them, CPU int32 [n]."""
+    nat = _native()
+    pages = nat.torch.empty((max(int(n), 0),), dtype=nat.i32)
+    _check(nat.call(nat.luvc_kv_take, _refs(refs), refs.numel(), int(n), pages.data_ptr() if n > 0 else None))
+    return pages
+
+
+def luvc_kv_fork(cache: KvCache, refs, pages, length: int, n_children: int, stream=None):
+    """n_children sequences that go on from the `length` tokens in `pages` (host integers).  Returns their pages, CPU int32
+    [n_children, ceil(length / page_tokens)]."""
+    nat = _native()
+    _here(nat, cache)
+    assert refs.numel() == cache.n_pages
+    a, at, n = _host_ints(pages)
+    used = -(-int(length) // cache.page_tokens)
+    assert n >= used
+    children = nat.torch.empty((max(int(n_children), 0), max(used, 0)), dtype=nat.i32)
+    _check(nat.call(nat.luvc_kv_fork, cache.addr, _refs(refs), at, int(length), int(n_children), children.data_ptr(), nat.stream(stream)))
+    return children
+
+
+def luvc_kv_release(refs, pages):
+    """Every page of `pages` (host integers) counts one less in refs (CPU int32 [n_pages], changed in place)."""
+    nat = _native()
+    a, at, n = _host_ints(pages)
+    _check(nat.call(nat.luvc_kv_release, _refs(refs), refs.numel(), at, n))
 
 
 class LaunchProfile:
