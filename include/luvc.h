@@ -383,7 +383,7 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
  * and the output is rounded once.  The parts of a long sequence are joined in a fixed order: same input, same bits.
  * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype); any contents, one per call
  * in flight, also for calls in captured graphs.
- * Limits: n_seqs * n_q_heads < 2^24.
+ * Limits: n_seqs * n_q_heads < 2^24, max_tokens < 2^30.
  */
 size_t luvc_kv_attend_workspace_bytes(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens);
 luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q, int64_t q_stride, int n_q_heads, int n_seqs,

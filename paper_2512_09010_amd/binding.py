@@ -653,7 +653,7 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
     assert table.dim() == 2 and table.shape[0] == S and table.dtype == nat.i32 and table.is_contiguous()
     assert lengths.dtype == nat.i32 and lengths.is_contiguous() and lengths.numel() == S
     if max_tokens is None:
-        max_tokens = max(table.shape[1] * cache.page_tokens, 1)
+        max_tokens = min(max(table.shape[1] * cache.page_tokens, 1), (1 << 30) - 1)
     if workspace is None:
         need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
         workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)

@@ -90,6 +90,7 @@ static bool attend_sizes_ok(const luvc_kv_cache* cache, int n_seqs, int n_q_head
 {
     if (n_seqs < 1 || n_q_heads < 1 || max_tokens < 1) { set_error("n_seqs, n_q_heads and max_tokens must be positive (got %d, %d, %d)", n_seqs, n_q_heads, max_tokens); return false; }
     if (n_q_heads % cache->n_heads) { set_error("n_q_heads=%d is no multiple of the cache's %d heads", n_q_heads, cache->n_heads); return false; }
+    if (max_tokens >= (1 << 30)) { set_error("max_tokens must stay below 2^30"); return false; }
     if ((int64_t)n_seqs * n_q_heads >= ((int64_t)1 << 24)) { set_error("n_seqs * n_q_heads must stay below 2^24"); return false; }
     return true;
 }
