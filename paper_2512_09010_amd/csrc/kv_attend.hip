@@ -19,6 +19,7 @@
 //
 // The four wavefronts join through LDS.  A sequence longer than a run is joined by the workgroup of its runs that ends last, which adds
 // in the order of the runs; hand-over and arrival words as in spu_tiles.hpp.
+#include <cmath>
 #include <type_traits>
 
 #include "common.hpp"
@@ -49,13 +50,13 @@ constexpr int attend_waves(int dp) { return dp == 256 ? 4 : 8; }        // what 
 __device__ __forceinline__ float xor16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32, kWave); }
 
-// W words from channel d of a row of D on; SMALL: D is less than 16 bytes, zeros behind it
+// W words at a byte offset; SMALL: the row has D elements, fewer than 16 bytes hold, of which those from d on are taken, zeros behind them
 template <typename T, int W, bool SMALL>
-__device__ __forceinline__ void load_words(uint32_t* w, const T* rows, uint32_t row, int d, int D)
+__device__ __forceinline__ void load_words(uint32_t* w, const char* rows, uint32_t off, int d, int D)
 {
     if constexpr (!SMALL) {
         typedef typename kv_piece_t<T, W>::type piece;
-        const piece p = *(const piece*)(rows + (row + (uint32_t)d));
+        const piece p = *(const piece*)(rows + off);
 #pragma unroll
         for (int i = 0; i < W; ++i) w[i] = p[i];
     } else {
@@ -64,8 +65,8 @@ __device__ __forceinline__ void load_words(uint32_t* w, const T* rows, uint32_t 
 #pragma unroll
         for (int e = 0; e < W * 4 / (int)sizeof(T); ++e) {
             if (d + e >= D) continue;
-            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(((const float*)rows)[row + d + e]);
-            else w[e / 2] |= (uint32_t)((const uint16_t*)rows)[row + d + e] << (e % 2 * 16);
+            if constexpr (sizeof(T) == 4) w[e] = *(const uint32_t*)(rows + off + 4 * e);
+            else w[e / 2] |= (uint32_t)*(const uint16_t*)(rows + off + 2 * e) << (e % 2 * 16);
         }
     }
 }
@@ -77,22 +78,23 @@ struct KvWork {
     float* parts;                    // [rows, tiles, splits, cols, parts_row]
     tile_tag_t* words;               // [rows, tiles]
     tile_tag_t tag;
-    bool q_pieces;                   // queries in aligned 16-byte pieces
+    float scale;                     // of the logits, to powers of two; positive
+    int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
 
-// DP: channels with room (64, 128, 256)
-template <typename T, int DP, bool SMALL>
+// DP: channels with room (64, 128, 256); SIZED: the cache has sizes
+template <typename T, int DP, bool SMALL, bool SIZED>
 __global__ void __launch_bounds__(attend_waves(DP) * 64)
 kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, KvAttend a)
 {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int NW = attend_waves(DP), NT = NW * 64;
+    constexpr int ES = (int)sizeof(T), NW = attend_waves(DP), NT = NW * 64;
     constexpr int TILES = BF ? 2 : 1, TOK = 16 * TILES, STEP = NW * TOK;      // tokens of a wavefront's step, of the workgroup's
-    constexpr int KE = BF ? 8 : 4;                            // elements in 16 bytes
+    constexpr int KE = 16 / ES;                               // elements in 16 bytes
     constexpr int NK = DP / (4 * KE);                         // pieces of a key per lane
-    constexpr int VL = DP == 64 ? 4 : KE, VW = VL * (int)sizeof(T) / 4, NV = DP / (16 * VL);      // of a value: elements, words, pieces
+    constexpr int VL = DP == 64 ? 4 : KE, VW = VL * ES / 4, NV = DP / (16 * VL);      // of a value: elements, words, pieces
     constexpr int VT = 4 * TILES;                             // tokens of a lane's part of the second sum
-    constexpr int LD = DP + 4, QLD = DP + KE;                 // rows in LDS
+    constexpr int LD = DP + 4, PIECES = DP / KE;              // a row of outputs in LDS; pieces of a query
     extern __shared__ __align__(16) float lds[];
     __shared__ float sm[NW][16], sl[NW][16];
     __shared__ int last_flag;
@@ -105,41 +107,39 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     const int64_t row = (int64_t)band * 8 + in_band % 8;
     if (row >= wk.rows) return;
     const int h = (int)(row % wk.n_heads), s = (int)(row / wk.n_heads);
-    const int split = blockIdx.y, D = wk.D, P1 = (1 << wk.log2_page) - 1;
+    const int split = blockIdx.y, D = wk.D;
 
     // what does not depend on one another is asked for together: the length, the first pages, the queries
-    int64_t most = (int64_t)a.max_pages << wk.log2_page;
-    const int room = most < a.max_tokens ? (int)most : a.max_tokens;
+    const int64_t held = (int64_t)a.max_pages << wk.log2_page;
+    const int room = held < a.max_tokens ? (int)held : a.max_tokens;
     const scalar_words table = as_scalars(a.table) + (int64_t)s * a.max_pages;
     int t0 = split * wk.chunk + wave * TOK;
     int now[TILES], next[TILES];
-    auto pages_at = [&](int t, int* pages) {
+    auto pages_at = [&](int t, int* pages) {                  // behind the end any page will do: its tokens are not live
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) pages[i] = t + 16 * i < room ? table[(t + 16 * i) >> wk.log2_page] : -1;
+        for (int i = 0; i < TILES; ++i) pages[i] = table[(t + 16 * i < room ? t + 16 * i : room - 1) >> wk.log2_page];
     };
     pages_at(t0, now);
     pages_at(t0 + STEP, next);
     int len = as_scalars(a.lengths)[s];
-    // query heads head0 .. head0 + nh - 1 of the call are columns of the products, zeros behind them
+    // Query heads head0 .. head0 + nh - 1 of the call are columns of the products, zeros behind them.  A piece that would reach beyond a
+    // row, of queries, keys or values, is the row's last one instead: what it repeats is zero among the queries, and of the values
+    // it makes the same channels of the output once more.
     const int head0 = h * wk.group + qt * wk.cols, left = wk.group - qt * wk.cols, nh = left < wk.cols ? left : wk.cols;
-    T* qs = (T*)lds;
-    const T* q0 = (const T*)a.q + s * a.q_stride + (int64_t)head0 * D;
-    if (wk.q_pieces) {
-        constexpr int PIECES = DP / KE;
-        for (int i = tid; i < 16 * PIECES; i += NT) {
-            const int col = i / PIECES, d = i % PIECES * KE;
-            kv_u32x4 w = {};
-            if (col < nh && d < D) w = *(const kv_u32x4*)(q0 + col * D + d);
-            *(kv_u32x4*)&qs[col * QLD + d] = w;
+    const char* q0 = (const char*)((const T*)a.q + s * a.q_stride + (int64_t)head0 * D);
+    for (int i = tid; i < 16 * PIECES; i += NT) {
+        const int col = i / PIECES, d0 = i % PIECES * KE, d1 = SMALL ? 0 : d0 < D - KE ? d0 : D - KE;
+        uint32_t w[4] = {};
+        if (col < nh && d0 < D && wk.sign) {
+            load_words<T, 4, SMALL>(w, q0, (uint32_t)((col * D + d1) * ES), d1, D);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (BF) w[e] &= (d1 + 2 * e >= d0 ? 0xffffu : 0u) | (d1 + 2 * e + 1 >= d0 ? 0xffff0000u : 0u);
+                else w[e] &= d1 + e >= d0 ? 0xffffffffu : 0u;
+                w[e] ^= wk.sign < 0 ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+            }
         }
-    } else {
-#pragma unroll 1
-        for (int i = tid; i < 16 * DP; i += NT) {
-            const int col = i / DP, d = i % DP;
-            T w{};
-            if (col < nh && d < D) w = q0[col * D + d];
-            qs[col * QLD + d] = w;
-        }
+        *(kv_u32x4*)&lds[(col * (PIECES + 1) + i % PIECES) * 4] = kv_u32x4{w[0], w[1], w[2], w[3]};
     }
     len = len < 0 ? 0 : len > room ? room : len;
     const int splits = len > wk.chunk ? (len + wk.chunk - 1) / wk.chunk : 1;
@@ -149,91 +149,63 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     if (splits > 1 && tid == 0) seen = tag_load(word);
     const int end = split == splits - 1 ? len : (split + 1) * wk.chunk;
 
-    // A piece that would reach beyond the row is the row's last one instead: what it repeats meets zeros among the queries, or is the
-    // same channel of the output once more
     uint32_t kf[TILES][NK][4], vf[VT][NV][VW];
     kv_sizes4 sz[TILES];
-    auto place = [&](int t, int page) -> int64_t {            // page and row as places of a head's tokens in the pool
-        page = page >= 0 && page < wk.n_pages ? page : 0;
-        return (((int64_t)page * wk.n_heads + h) << wk.log2_page) + (t & P1);
-    };
+    uint32_t k_off[NK], v_off[4][NV];                         // bytes from the first row of a tile
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+        const int d = (4 * n + g) * KE;
+        k_off[n] = (uint32_t)((c * D + (SMALL ? 0 : d < D - KE ? d : D - KE)) * ES);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int d = (16 * n + c) * VL;
+            v_off[j][n] = (uint32_t)(((4 * g + j) * D + (SMALL || d < D - VL ? d : D - VL)) * ES);
+        }
+    const uint32_t row_bytes = (uint32_t)(D * ES), P1 = (1u << wk.log2_page) - 1, page_bytes = (uint32_t)wk.n_heads * row_bytes << wk.log2_page;
+    const char* const k0 = (const char*)kpool + ((uint64_t)h * row_bytes << wk.log2_page);
+    const char* const v0 = (const char*)vpool + ((uint64_t)h * row_bytes << wk.log2_page);
+    uint64_t tile[TILES];                                     // bytes to the tiles of the step that is asked for
     auto ask_keys = [&](int t, const int* pages) {
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const T* rows = kpool + place(t + 16 * i, pages[i]) * D;
+        for (int i = 0; i < TILES; ++i) {                     // without a page, page 0: its tokens are then not live
+            const uint32_t p = (uint32_t)pages[i] < (uint32_t)wk.n_pages ? pages[i] : 0, r = (uint32_t)(t + 16 * i) & P1;
+            tile[i] = (uint64_t)p * page_bytes + r * row_bytes;
 #pragma unroll
-            for (int n = 0; n < NK; ++n) {
-                int d = (4 * n + g) * KE;
-                d = SMALL ? 0 : d < D - KE ? d : D - KE;
-                load_words<T, 4, SMALL>(kf[i][n], rows, (uint32_t)(c * D), d, D);
-            }
-            if (wk.sizes) {
-                const int page = pages[i] >= 0 && pages[i] < wk.n_pages ? pages[i] : 0;
-                sz[i] = *(const kv_sizes4*)(wk.sizes + (((int64_t)page << wk.log2_page) + ((t + 16 * i) & P1)) + 4 * g);
-            }
+            for (int n = 0; n < NK; ++n) load_words<T, 4, SMALL>(kf[i][n], k0 + tile[i], k_off[n], 0, D);
+            if constexpr (SIZED) sz[i] = *(const kv_sizes4*)((const char*)(wk.sizes + (((uint64_t)p << wk.log2_page) + r)) + 16u * g);
         }
     };
-    auto ask_values = [&](int t, const int* pages) {
+    auto ask_values = [&]() {
 #pragma unroll
-        for (int j = 0; j < VT; ++j) {
-            const T* rows = vpool + (place(t + 16 * (j / 4), pages[j / 4]) + j % 4) * D;
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                int d = (16 * n + c) * VL;
-                d = SMALL || d < D - VL ? d : D - VL;
-                load_words<T, VW, SMALL>(vf[j][n], rows, (uint32_t)(4 * g * D), d, D);
-            }
-        }
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int n = 0; n < NV; ++n) load_words<T, VW, SMALL>(vf[4 * i + j][n], v0 + tile[i], v_off[j][n], (16 * n + c) * VL, D);
     };
     if (t0 < end) {
         ask_keys(t0, now);
-        ask_values(t0, now);
+        ask_values();
     }
     __syncthreads();                                          // the queries are in LDS
     uint32_t qf[NK][4];
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
-        const int d0 = (4 * n + g) * KE, d1 = SMALL ? 0 : d0 < D - KE ? d0 : D - KE;
-        if (d1 == d0) {
-            const kv_u32x4 w = *(const kv_u32x4*)&qs[c * QLD + d0];
+        const kv_u32x4 w = *(const kv_u32x4*)&lds[(c * (PIECES + 1) + 4 * n + g) * 4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[n][i] = w[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (BF) {
-                    const int e = d1 + 2 * i;
-                    qf[n][i] = (e >= d0 && e < D ? ((const uint16_t*)qs)[c * QLD + e] : 0u) | (e + 1 >= d0 && e + 1 < D ? (uint32_t)((const uint16_t*)qs)[c * QLD + e + 1] << 16 : 0u);
-                } else {
-                    const int e = d1 + i;
-                    qf[n][i] = e >= d0 && e < D ? ((const uint32_t*)qs)[c * QLD + e] : 0u;
-                }
-            }
-        }
+        for (int i = 0; i < 4; ++i) qf[n][i] = w[i];
     }
 
     kv_f32x4 o[NV * VL] = {};
     float m = kLowest, l = 0.f, ls = 0.f;
-    const float scale = a.scale * kLogE;
-    for (; t0 < end; t0 += STEP) {
-        uint32_t live = 0;                                    // a bit for each of the lane's tokens
-        float lg[VT] = {};
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int n = now[i] >= 0 && now[i] < wk.n_pages ? end - (t0 + 16 * i + 4 * g) : 0;
-            live |= (n >= 4 ? 15u : n > 0 ? (1u << n) - 1u : 0u) << (4 * i);
-            if (wk.sizes) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (sz[i][e] < 1) live &= ~(1u << (4 * i + e));
-                    if (a.enhance) lg[4 * i + e] = __log2f((float)(sz[i][e] < 1 ? 1 : sz[i][e]));
-                }
-            }
-        }
-        constexpr uint32_t ALL = (1u << VT) - 1u;
-        const bool whole = __all(live == ALL);
-
-        // logits, in powers of two
+    // MORE: the next step's keys take the place of this one's while the weights are formed, its values that of the values after them.
+    // A step without a successor is code of its own: with the requests behind a condition, the wait for the values would have to be one
+    // for everything in flight.
+    auto step = [&](auto MORE) {
+        // logits but for the scale
         float p[VT];
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
@@ -248,13 +220,33 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[4 * i + e] = z[e] * scale;
+            for (int e = 0; e < 4; ++e) p[4 * i + e] = z[e];
         }
-        // the next step's keys take the place of these while the weights are formed, its values that of the values after them
-        const int tn = t0 + STEP;
+        bool whole = !SIZED && t0 + TOK <= end;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) whole = whole && (uint32_t)now[i] < (uint32_t)wk.n_pages;
+        uint32_t live = 0;                                    // a bit for each of the lane's tokens
+        float lg[VT] = {};
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const int n = (uint32_t)now[i] < (uint32_t)wk.n_pages ? end - (t0 + 16 * i + 4 * g) : 0;
+                live |= (n >= 4 ? 15u : n > 0 ? (1u << n) - 1u : 0u) << (4 * i);
+                if constexpr (SIZED) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (sz[i][e] < 1) live &= ~(1u << (4 * i + e));
+                        if (a.enhance) lg[4 * i + e] = __log2f((float)(sz[i][e] < 1 ? 1 : sz[i][e]));
+                    }
+                }
+            }
+            whole = __all(live == (1u << VT) - 1u);
+        }
         int after[TILES];
-        pages_at(tn + STEP, after);
-        if (tn < end) ask_keys(tn, next);
+        if constexpr (MORE) {
+            pages_at(t0 + 2 * STEP, after);
+            ask_keys(t0 + STEP, next);
+        }
         if (!whole) {
 #pragma unroll
             for (int j = 0; j < VT; ++j) p[j] = live >> j & 1 ? p[j] : -__builtin_inff();
@@ -262,6 +254,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         float top = p[0];
 #pragma unroll
         for (int j = 1; j < VT; ++j) top = fmaxf(top, p[j]);
+        top *= wk.scale;
         if (__any(top > m + 8.f)) {
             top = fmaxf(top, xor16(top));
             top = fmaxf(top, xor32(top));
@@ -275,9 +268,12 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         }
 #pragma unroll
         for (int j = 0; j < VT; ++j) {
-            p[j] = __builtin_amdgcn_exp2f(p[j] - m);
+            p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], wk.scale, -m));
             l += p[j];
-            ls += p[j] * lg[j];
+        }
+        if constexpr (SIZED) {
+#pragma unroll
+            for (int j = 0; j < VT; ++j) ls += p[j] * lg[j];
         }
         if (!whole) {
 #pragma unroll
@@ -314,10 +310,14 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                     for (int j = 0; j < VT; ++j)
                         o[n * VL + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[j][n][e]), p[j], o[n * VL + e], 0, 0, 0);
         }
-        if (tn < end) ask_values(tn, next);
+        if constexpr (MORE) {
+            ask_values();
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) { now[i] = next[i]; next[i] = after[i]; }
-    }
+            for (int i = 0; i < TILES; ++i) { now[i] = next[i]; next[i] = after[i]; }
+        }
+    };
+    for (; t0 + STEP < end; t0 += STEP) step(std::true_type{});
+    if (t0 < end) step(std::false_type{});
 
     // ---- the wavefronts' parts; log s goes to every channel
     l += xor16(l);
@@ -354,11 +354,20 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, splits * part * 4, 0x00020000);
     auto store = [&](int col, int d, kv_f32x4 v) {
         T* out = (T*)a.out + s * a.out_stride + (int64_t)(head0 + col) * D + d;
+        if (d + 4 <= D) {
+            if constexpr (BF) {
+                typedef uint16_t quad __attribute__((ext_vector_type(4), aligned(2)));
+                *(quad*)out = quad{f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
+            } else {
+                *(kv_f32x4u*)out = v;
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (d + i >= D) continue;
-            if constexpr (BF) out[i].bits = f32_to_bf16(v[i]);
-            else out[i] = v[i];
+            for (int i = 0; i < 3; ++i) {
+                if (d + i >= D) continue;
+                if constexpr (BF) out[i].bits = f32_to_bf16(v[i]);
+                else out[i] = v[i];
+            }
         }
     };
     for (int i = tid; i < items; i += NT) {
@@ -390,60 +399,54 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     if (tid == 0) last_flag = tiles_arrive(word, splits);
     __syncthreads();
     if (!last_flag) return;
-    float *weight = lds, *total = sl[0], *red = lds + kMaxSplits * 16;      // [splits][cols], [cols], [NT][4]
+    float *weight = lds, *total = sl[0], *red = lds + kMaxSplits * 16;      // [splits][16], [cols], [NT][4]
     // Few channels in all: several threads to four of them, each with every groups-th run.  The first AHEAD runs of a thread are asked for
     // together with the maxima and sums that their weights are formed of.
     constexpr int AHEAD = 16;
     const int groups = items < NT ? NT / items : 1;
-    const int lane_item = groups > 1 ? tid % items : tid, grp = groups > 1 ? tid / items : 0;
-    kv_f32x4 x[AHEAD];
-    auto ask = [&](int i, int k0) {
-        const int col = i / quads, d = i % quads * 4;
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int run = k0 + k * groups;
-            if (run < splits) x[k] = __builtin_bit_cast(kv_f32x4, tile_vec<4>::load(all, (uint32_t)((run * part + col * wk.parts_row + d) * 4)));
-        }
-    };
-    const bool mine = lane_item < items && grp < groups;
-    if (mine) ask(lane_item, grp);
-    for (int col = wave; col < nh; col += NW) {
-        float mx[kMaxSplits / 64], sx[kMaxSplits / 64], top = kLowest, sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < kMaxSplits / 64; ++k) {
-            const int i = lane + 64 * k;
-            mx[k] = kLowest;
-            sx[k] = 0.f;
-            if (i < splits) {
-                const tile_vec<4>::type w = tile_vec<4>::load(all, (uint32_t)((i * part + (col + 1) * wk.parts_row - 4) * 4));
-                mx[k] = __uint_as_float(w[0]);
-                sx[k] = __uint_as_float(w[1]);
-            }
-            top = fmaxf(top, mx[k]);
-        }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
-#pragma unroll
-        for (int k = 0; k < kMaxSplits / 64; ++k) {
-            const int i = lane + 64 * k;
-            const float f = __builtin_amdgcn_exp2f(mx[k] - top);
-            sum += f * sx[k];
-            if (i < splits) weight[i * 16 + col] = f;
-        }
-        sum = wave_sum(sum);
-        if (lane == 0) total[col] = sum > 0.f ? 1.f / sum : 0.f;
-    }
-    __syncthreads();
+    const int item0 = groups > 1 ? tid % items : tid, grp = groups > 1 ? tid / items : 0;
     for (int i0 = 0; i0 < items; i0 += NT) {
-        const int i = i0 + lane_item, col = i / quads;
+        const int i = i0 + item0, col = i / quads, d = i % quads * 4;
         const bool in = i < items && grp < groups;
-        if (in && i0) ask(i, grp);
         kv_f32x4 v = {};
-        for (int k0 = grp; in && k0 < splits; k0 += AHEAD * groups) {
-            if (k0 != grp) ask(i, k0);
+        for (int k0 = 0; k0 < splits; k0 += AHEAD * groups) {
+            tile_vec<4>::type x[AHEAD];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-                if (k0 + k * groups < splits) v += weight[(k0 + k * groups) * 16 + col] * x[k];
+            for (int k = 0; k < AHEAD; ++k) {
+                const int run = k0 + k * groups + grp;
+                x[k] = tile_vec<4>::load(all, (uint32_t)(((in && run < splits ? run : 0) * part + (in ? col * wk.parts_row + d : 0)) * 4));
+            }
+            if (i0 == 0 && k0 == 0) {
+#pragma unroll 1
+                for (int u = wave; u < nh; u += NW) {
+                    float mx[kMaxSplits / 64], sx[kMaxSplits / 64], top = kLowest, sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < kMaxSplits / 64; ++k) {
+                        const int r = lane + 64 * k;
+                        const tile_vec<4>::type w = tile_vec<4>::load(all, (uint32_t)(((r < splits ? r : 0) * part + (u + 1) * wk.parts_row - 4) * 4));
+                        mx[k] = r < splits ? __uint_as_float(w[0]) : kLowest;
+                        sx[k] = r < splits ? __uint_as_float(w[1]) : 0.f;
+                        top = fmaxf(top, mx[k]);
+                    }
+#pragma unroll
+                    for (int b = 32; b > 0; b >>= 1) top = fmaxf(top, __shfl_xor(top, b, kWave));
+#pragma unroll
+                    for (int k = 0; k < kMaxSplits / 64; ++k) {
+                        const float f = __builtin_amdgcn_exp2f(mx[k] - top);
+                        sum += f * sx[k];
+                        if (lane + 64 * k < splits) weight[(lane + 64 * k) * 16 + u] = f;
+                    }
+                    sum = wave_sum(sum);
+                    if (lane == 0) total[u] = sum > 0.f ? 1.f / sum : 0.f;
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int run = k0 + k * groups + grp;
+                const float f = in && run < splits ? weight[run * 16 + col] : 0.f;
+                v += f * __builtin_bit_cast(kv_f32x4, x[k]);
+            }
         }
         if (groups > 1) {
             *(kv_f32x4*)&red[tid * 4] = v;
@@ -451,7 +454,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             if (in && grp == 0)
                 for (int k = 1; k < groups; ++k) v += *(const kv_f32x4*)&red[(k * items + i) * 4];
         }
-        if (in && grp == 0) store(col, i % quads * 4, v * total[col]);
+        if (in && grp == 0) store(col, d, v * total[col]);
     }
 }
 
@@ -492,8 +495,10 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
 template <typename T, int DP, bool SMALL>
 void attend_launch(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
-    LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL>), dim3(p.blocks, p.splits), dim3(attend_waves(DP) * 64), p.lds, st,
-                (const T*)c.k + layer * c.layer_stride, (const T*)c.v + layer * c.layer_stride, wk, a);
+    const T *k = (const T*)c.k + layer * c.layer_stride, *v = (const T*)c.v + layer * c.layer_stride;
+    const dim3 grid(p.blocks, p.splits), block(attend_waves(DP) * 64);
+    if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
+    else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
 }
 
 template <typename T>
@@ -515,10 +520,9 @@ size_t kv_attend_workspace(int n_seqs, int n_q_heads, int n_heads, int D, luvc_d
 luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, void* ws, hipStream_t st)
 {
     const AttendPlan p = attend_plan(a.n_seqs, a.n_q_heads, c.n_heads, c.D, c.dtype, a.max_tokens);
-    const int64_t es = (int64_t)kv_esize(c);
-    const bool q_pieces = (c.D * es) % 16 == 0 && ((uintptr_t)a.q | (uint64_t)(a.q_stride * es)) % 16 == 0;
     const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.rows,
-                    (float*)((char*)ws + p.words), (tile_tag_t*)ws, spu_next_tag(), q_pieces};
+                    (float*)((char*)ws + p.words), (tile_tag_t*)ws, spu_next_tag(),
+                    a.scale == 0.f ? 1.f : std::fabs(a.scale) * kLogE, a.scale < 0.f ? -1 : a.scale > 0.f};
     if (c.dtype == LUVC_F32) attend_shape<float>(p, c, layer, wk, a, st);
     else attend_shape<bf16_t>(p, c, layer, wk, a, st);
     return check_launch("attention over the cache");
