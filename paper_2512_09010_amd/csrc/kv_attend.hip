@@ -19,6 +19,7 @@
 //
 // The four wavefronts join through LDS.  A sequence longer than a run is joined by the workgroup of its runs that ends last, which adds
 // in the order of the runs; hand-over and arrival words as in spu_tiles.hpp.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -45,7 +46,7 @@ constexpr int kMaxSplits = 256;
 constexpr float kLogE = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
-constexpr int attend_waves(int dp) { return dp == 256 ? 4 : 8; }        // what registers allow to be resident at two, one per SIMD
+constexpr int kWaves = 4;
 
 __device__ __forceinline__ float xor16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32, kWave); }
@@ -74,7 +75,8 @@ __device__ __forceinline__ void load_words(uint32_t* w, const char* rows, uint32
 struct KvWork {
     const int32_t* sizes;
     int n_pages, n_heads, log2_page, D, group, chunk, tiles, cols, parts_row;      // tiles of at most `cols` query heads; parts_row: floats
-    int64_t rows;                    // sequences x cache heads
+    int lds_words;                   // where the maxima and sums of the wavefronts lie in LDS
+    unsigned rows, splits;           // sequences x cache heads; the most runs of one
     float* parts;                    // [rows, tiles, splits, cols, parts_row]
     tile_tag_t* words;               // [rows, tiles]
     tile_tag_t tag;
@@ -82,32 +84,33 @@ struct KvWork {
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
 
-// DP: channels with room (64, 128, 256); SIZED: the cache has sizes
+// DP: channels with room (64, 128, 256); SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
 template <typename T, int DP, bool SMALL, bool SIZED>
-__global__ void __launch_bounds__(attend_waves(DP) * 64)
+__global__ void __launch_bounds__(kWaves * 64, DP == 256 ? 1 : DP == 64 ? 4 : sizeof(T) == 4 ? 2 : 3)
 kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, KvAttend a)
 {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int ES = (int)sizeof(T), NW = attend_waves(DP), NT = NW * 64;
+    constexpr int ES = (int)sizeof(T), NW = kWaves, NT = NW * 64;
     constexpr int TILES = BF ? 2 : 1, TOK = 16 * TILES, STEP = NW * TOK;      // tokens of a wavefront's step, of the workgroup's
     constexpr int KE = 16 / ES;                               // elements in 16 bytes
     constexpr int NK = DP / (4 * KE);                         // pieces of a key per lane
     constexpr int VL = DP == 64 ? 4 : KE, VW = VL * ES / 4, NV = DP / (16 * VL);      // of a value: elements, words, pieces
     constexpr int VT = 4 * TILES;                             // tokens of a lane's part of the second sum
-    constexpr int LD = DP + 4, PIECES = DP / KE;              // a row of outputs in LDS; pieces of a query
-    extern __shared__ __align__(16) float lds[];
-    __shared__ float sm[NW][16], sl[NW][16];
-    __shared__ int last_flag;
+    constexpr int LD = DP + 4, PIECES = DP / KE;              // a row of outputs in LDS; pieces of a query or a key
+    constexpr int KU = PIECES / 4, SWZ = PIECES < 16 ? PIECES - 1 : 15;       // loads of a tile of keys, 64 pieces each
+    // In LDS, one after the other: the wavefronts' keys, queries; then parts of the outputs; then weights and partial sums of the join
+    extern __shared__ __align__(16) char lds[];
+    float(*sm)[16] = (float(*)[16])(lds + wk.lds_words), (*sl)[16] = sm + NW;
+    int& last_flag = *(int*)(sl + NW);
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // tiles of one sequence and cache head read the same rows: eight workgroups apart they meet in the L2 of one XCD
-    const unsigned band = blockIdx.x / (8 * wk.tiles), in_band = blockIdx.x % (8 * wk.tiles);
-    const int qt = in_band / 8;
-    const int64_t row = (int64_t)band * 8 + in_band % 8;
-    if (row >= wk.rows) return;
-    const int h = (int)(row % wk.n_heads), s = (int)(row / wk.n_heads);
-    const int split = blockIdx.y, D = wk.D;
+    // runs before rows, so that long sequences' later runs come last; tiles of one run read the same tokens: eight workgroups apart they
+    // meet in the L2 of one XCD
+    const unsigned band = blockIdx.x / (8 * wk.tiles), in_band = blockIdx.x % (8 * wk.tiles), unit = band * 8 + in_band % 8;
+    const int qt = in_band / 8, split = unit / wk.rows, row = unit % wk.rows;
+    if (unit >= wk.rows * wk.splits) return;
+    const int h = row % wk.n_heads, s = row / wk.n_heads, D = wk.D;
 
     // what does not depend on one another is asked for together: the length, the first pages, the queries
     const int64_t held = (int64_t)a.max_pages << wk.log2_page;
@@ -126,6 +129,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     // row, of queries, keys or values, is the row's last one instead: what it repeats is zero among the queries, and of the values
     // it makes the same channels of the output once more.
     const int head0 = h * wk.group + qt * wk.cols, left = wk.group - qt * wk.cols, nh = left < wk.cols ? left : wk.cols;
+    char* const queries = lds + NW * TOK * PIECES * 16;
     const char* q0 = (const char*)((const T*)a.q + s * a.q_stride + (int64_t)head0 * D);
     for (int i = tid; i < 16 * PIECES; i += NT) {
         const int col = i / PIECES, d0 = i % PIECES * KE, d1 = SMALL ? 0 : d0 < D - KE ? d0 : D - KE;
@@ -139,23 +143,27 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                 w[e] ^= wk.sign < 0 ? (BF ? 0x80008000u : 0x80000000u) : 0u;
             }
         }
-        *(kv_u32x4*)&lds[(col * (PIECES + 1) + i % PIECES) * 4] = kv_u32x4{w[0], w[1], w[2], w[3]};
+        *(kv_u32x4*)(queries + (col * (PIECES + 1) + i % PIECES) * 16) = kv_u32x4{w[0], w[1], w[2], w[3]};
     }
     len = len < 0 ? 0 : len > room ? room : len;
     const int splits = len > wk.chunk ? (len + wk.chunk - 1) / wk.chunk : 1;
     if (split >= splits) return;
-    tile_tag_t* word = wk.words + (row * wk.tiles + qt);
+    tile_tag_t* word = wk.words + ((int64_t)row * wk.tiles + qt);
     tile_tag_t seen = 0;
     if (splits > 1 && tid == 0) seen = tag_load(word);
     const int end = split == splits - 1 ? len : (split + 1) * wk.chunk;
 
-    uint32_t kf[TILES][NK][4], vf[VT][NV][VW];
+    // Keys as the product wants them, 16 bytes of one token per lane and the tokens in neighbouring lanes, would be 64 places to look
+    // up per load; as neighbouring lanes read them here, rows, they are 16 or fewer, and LDS turns them round.  Piece p of row r lies at
+    // p ^ (r % 16) of its row there, so that the 16 rows of one read meet different banks.
+    uint32_t kr[TILES][KU][4], vf[VT][NV][VW];
     kv_sizes4 sz[TILES];
-    uint32_t k_off[NK], v_off[4][NV];                         // bytes from the first row of a tile
+    uint32_t k_off[KU], v_off[4][NV];                         // bytes from the first row of a tile
+    char* const keys = lds + wave * (TOK * PIECES * 16);
 #pragma unroll
-    for (int n = 0; n < NK; ++n) {
-        const int d = (4 * n + g) * KE;
-        k_off[n] = (uint32_t)((c * D + (SMALL ? 0 : d < D - KE ? d : D - KE)) * ES);
+    for (int u = 0; u < KU; ++u) {
+        const int r = (64 * u + lane) / PIECES, d = ((lane % PIECES) ^ (r & SWZ)) * KE;
+        k_off[u] = (uint32_t)((r * D + (SMALL ? 0 : d < D - KE ? d : D - KE)) * ES);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -174,11 +182,17 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             const uint32_t p = (uint32_t)pages[i] < (uint32_t)wk.n_pages ? pages[i] : 0, r = (uint32_t)(t + 16 * i) & P1;
             tile[i] = (uint64_t)p * page_bytes + r * row_bytes;
 #pragma unroll
-            for (int n = 0; n < NK; ++n) load_words<T, 4, SMALL>(kf[i][n], k0 + tile[i], k_off[n], 0, D);
-            if constexpr (SIZED) sz[i] = *(const kv_sizes4*)((const char*)(wk.sizes + (((uint64_t)p << wk.log2_page) + r)) + 16u * g);
+            for (int u = 0; u < KU; ++u) load_words<T, 4, SMALL>(kr[i][u], k0 + tile[i], k_off[u], ((lane % PIECES) ^ (((64 * u + lane) / PIECES) & SWZ)) * KE, D);
         }
     };
-    auto ask_values = [&]() {
+    auto ask_values = [&](int t, const int* pages) {
+        if constexpr (SIZED) {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const uint32_t p = (uint32_t)pages[i] < (uint32_t)wk.n_pages ? pages[i] : 0;
+                sz[i] = *(const kv_sizes4*)((const char*)(wk.sizes + (((uint64_t)p << wk.log2_page) + ((uint32_t)(t + 16 * i) & P1))) + 16u * g);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
@@ -188,13 +202,13 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     };
     if (t0 < end) {
         ask_keys(t0, now);
-        ask_values();
+        ask_values(t0, now);
     }
     __syncthreads();                                          // the queries are in LDS
     uint32_t qf[NK][4];
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
-        const kv_u32x4 w = *(const kv_u32x4*)&lds[(c * (PIECES + 1) + 4 * n + g) * 4];
+        const kv_u32x4 w = *(const kv_u32x4*)(queries + (c * (PIECES + 1) + 4 * n + g) * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) qf[n][i] = w[i];
     }
@@ -205,6 +219,12 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     // A step without a successor is code of its own: with the requests behind a condition, the wait for the values would have to be one
     // for everything in flight.
     auto step = [&](auto MORE) {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int u = 0; u < KU; ++u)
+                *(kv_u32x4*)(keys + (i * 16 * PIECES + 64 * u + lane) * 16) = kv_u32x4{kr[i][u][0], kr[i][u][1], kr[i][u][2], kr[i][u][3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         // logits but for the scale
         float p[VT];
 #pragma unroll
@@ -212,11 +232,12 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             kv_f32x4 z = {};
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
+                const kv_u32x4 kf = *(const kv_u32x4*)(keys + (i * 16 + c) * PIECES * 16 + (((4 * n + g) ^ (c & SWZ)) * 16));
                 if constexpr (BF) {
-                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_bf16x8, *(kv_u32x4*)kf[i][n]), __builtin_bit_cast(kv_bf16x8, *(kv_u32x4*)qf[n]), z, 0, 0, 0);
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_bf16x8, kf), __builtin_bit_cast(kv_bf16x8, *(kv_u32x4*)qf[n]), z, 0, 0, 0);
                 } else {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][n][w]), __uint_as_float(qf[n][w]), z, 0, 0, 0);
+                    for (int w = 0; w < 4; ++w) z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[w]), __uint_as_float(qf[n][w]), z, 0, 0, 0);
                 }
             }
 #pragma unroll
@@ -311,7 +332,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                         o[n * VL + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[j][n][e]), p[j], o[n * VL + e], 0, 0, 0);
         }
         if constexpr (MORE) {
-            ask_values();
+            ask_values(t0 + STEP, next);
 #pragma unroll
             for (int i = 0; i < TILES; ++i) { now[i] = next[i]; next[i] = after[i]; }
         }
@@ -326,7 +347,8 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     ls += xor32(ls);
     ls *= kLn2;
     if (g == 0) { sm[wave][c] = m; sl[wave][c] = l; }
-    __syncthreads();                                          // the queries have been read
+    __syncthreads();                                          // queries and keys have been read
+    float* const so = (float*)lds;
     if (c < nh) {
 #pragma unroll
         for (int n = 0; n < NV; ++n)
@@ -340,7 +362,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                     kv_f32x4u w;
 #pragma unroll
                     for (int b = 0; b < 4; ++b) w[b] = o[n * VL + e + b][i] + ls;
-                    *(kv_f32x4u*)&lds[(wave * wk.cols + c) * LD + d + e] = w;
+                    *(kv_f32x4u*)&so[(wave * wk.cols + c) * LD + d + e] = w;
                 }
             }
     }
@@ -350,7 +372,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     }
     __syncthreads();
     const int quads = (D + 3) / 4, items = nh * quads, part = wk.cols * wk.parts_row;
-    float* parts = wk.parts + (row * wk.tiles + qt) * gridDim.y * part;
+    float* parts = wk.parts + ((int64_t)row * wk.tiles + qt) * wk.splits * part;
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, splits * part * 4, 0x00020000);
     auto store = [&](int col, int d, kv_f32x4 v) {
         T* out = (T*)a.out + s * a.out_stride + (int64_t)(head0 + col) * D + d;
@@ -381,7 +403,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         for (int w = 0; w < NW; ++w) {
             const float f = __builtin_amdgcn_exp2f(sm[w][col] - top);
             sum += f * sl[w][col];
-            v += f * *(const kv_f32x4*)&lds[(w * wk.cols + col) * LD + d];
+            v += f * *(const kv_f32x4*)&so[(w * wk.cols + col) * LD + d];
         }
         if (splits == 1) {
             store(col, d, v * (sum > 0.f ? 1.f / sum : 0.f));
@@ -396,10 +418,14 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     // ---- the runs of the sequence, by the workgroup that ends last
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) last_flag = tiles_arrive(word, splits);
+    if (tid == 0) {
+        const tile_tag_t old = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last_flag = (int)(old & 0xffffu) == splits - 1;
+        if (last_flag) tag_store(word, wk.tag << 16);
+    }
     __syncthreads();
     if (!last_flag) return;
-    float *weight = lds, *total = sl[0], *red = lds + kMaxSplits * 16;      // [splits][16], [cols], [NT][4]
+    float *weight = so, *total = sl[0], *red = so + kMaxSplits * 16;      // [splits][16], [cols], [NT][4]
     // Few channels in all: several threads to four of them, each with every groups-th run.  The first AHEAD runs of a thread are asked for
     // together with the maxima and sums that their weights are formed of.
     constexpr int AHEAD = 16;
@@ -458,9 +484,31 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     }
 }
 
+// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  Joining runs costs 4 us
+// behind the last one and 0.6 for every further trip to memory of the join; a workgroup that is alone on its unit takes a step in
+// 1.2 us as long as memory keeps up with all of them, which it does to 5.9 TB/s (all measured: 1 x 32768 tokens, 8 heads of 128, bf16,
+// 256 steps: 45.8 us with 32 steps to a workgroup, 30.5 with 16, 29.5 with 12, 30.8 with 8, 35.2 with 4, 61 with 2).  At most 8 (1024
+// tokens in bf16) where that leaves two workgroups to a unit: `all` is a bound, and one sequence of that length among short
+// ones would be waited for (64 sequences of 1 to 8200 tokens: 86 us with 16 steps, 76 with 8; 64 of 4096 lose 193 for 180).
+int attend_steps(int64_t tiles, int all, int quads, double step_bytes)
+{
+    const int64_t fewest = std::max<int64_t>((all + kMaxSplits - 1) / kMaxSplits, (tiles * all >> 22) + 1);
+    const int64_t most = tiles * ((all + 7) / 8) >= 512 ? 8 : all;
+    const int groups = quads < kWaves * 64 ? kWaves * 64 / quads : 1;
+    const double memory = (double)tiles * all * step_bytes / 5.9e6;
+    int64_t best = std::min<int64_t>(fewest, all);
+    double least = 1e300;
+    for (int64_t n = best; n <= std::min<int64_t>(most, all); n += n < 4 ? 1 : n / 4) {
+        const int64_t runs = (all + n - 1) / n, each = (tiles * runs + 255) / 256;
+        const double us = std::max(memory, n * (0.8 + 0.4 * each)) + (runs > 1 ? 4.0 + 0.6 * ((runs - 1) / (16 * groups)) : 0.0);
+        if (us < least) { least = us; best = n; }
+    }
+    return (int)best;
+}
+
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, tiles, cols, chunk, splits, parts_row;
+    int dp, tiles, cols, chunk, splits, parts_row, lds_words;
     int64_t rows;
     unsigned blocks;
     size_t words, bytes, lds;
@@ -473,22 +521,20 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.tiles = (group + 15) / 16;
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
-    p.blocks = (unsigned)((p.rows + 7) / 8 * 8 * p.tiles);
-    const int waves = attend_waves(p.dp), step = waves * (dt == LUVC_F32 ? 16 : 32);
-    const int64_t want = (512 + p.rows * p.tiles - 1) / (p.rows * p.tiles);
-    int64_t per = (max_tokens + want - 1) / want;
-    per = per < 1024 ? per : 1024;
-    if ((max_tokens + per - 1) / per > kMaxSplits) per = (max_tokens + kMaxSplits - 1) / kMaxSplits;
-    p.chunk = (int)((per + step - 1) / step * step);
+    const int waves = kWaves, step = waves * (dt == LUVC_F32 ? 16 : 32);
+    p.chunk = attend_steps(p.rows * p.tiles, (max_tokens + step - 1) / step, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
     p.splits = (max_tokens + p.chunk - 1) / p.chunk;
+    p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
     p.words = align_up((size_t)p.rows * p.tiles * sizeof(tile_tag_t));
     p.bytes = p.words + (p.splits > 1 ? align_up((size_t)p.rows * p.tiles * p.splits * p.cols * p.parts_row * sizeof(float)) : 0);
-    // queries; parts of the wavefronts; weights of the runs and partial sums over them
-    const size_t qs = (size_t)16 * (p.dp * es + 16), parts = (size_t)waves * p.cols * (p.dp + 4) * sizeof(float);
+    // keys and queries; parts of the wavefronts; weights of the runs and partial sums over them.  Then maxima, sums, a word
+    const size_t front = (size_t)(waves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)waves * p.cols * (p.dp + 4) * sizeof(float);
     const size_t join = p.splits > 1 ? (size_t)kMaxSplits * 16 * sizeof(float) + (size_t)waves * 64 * 16 : 0;
-    p.lds = qs > parts ? qs : parts;
-    p.lds = p.lds > join ? p.lds : join;
+    size_t most = front > parts ? front : parts;
+    most = most > join ? most : join;
+    p.lds_words = (int)align_up(most, 16);
+    p.lds = p.lds_words + (2 * (size_t)waves * 16 + 4) * sizeof(float);
     return p;
 }
 
@@ -496,7 +542,7 @@ template <typename T, int DP, bool SMALL>
 void attend_launch(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
     const T *k = (const T*)c.k + layer * c.layer_stride, *v = (const T*)c.v + layer * c.layer_stride;
-    const dim3 grid(p.blocks, p.splits), block(attend_waves(DP) * 64);
+    const dim3 grid(p.blocks), block(kWaves * 64);
     if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
     else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
 }
@@ -520,8 +566,9 @@ size_t kv_attend_workspace(int n_seqs, int n_q_heads, int n_heads, int D, luvc_d
 luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, void* ws, hipStream_t st)
 {
     const AttendPlan p = attend_plan(a.n_seqs, a.n_q_heads, c.n_heads, c.D, c.dtype, a.max_tokens);
-    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.rows,
-                    (float*)((char*)ws + p.words), (tile_tag_t*)ws, spu_next_tag(),
+    static const tile_tag_t tag = spu_next_tag();
+    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.lds_words, (unsigned)p.rows, (unsigned)p.splits,
+                    (float*)((char*)ws + p.words), (tile_tag_t*)ws, tag,
                     a.scale == 0.f ? 1.f : std::fabs(a.scale) * kLogE, a.scale < 0.f ? -1 : a.scale > 0.f};
     if (c.dtype == LUVC_F32) attend_shape<float>(p, c, layer, wk, a, st);
     else attend_shape<bf16_t>(p, c, layer, wk, a, st);
