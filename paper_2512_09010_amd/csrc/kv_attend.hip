@@ -117,13 +117,13 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     const int room = held < a.max_tokens ? (int)held : a.max_tokens;
     const scalar_words table = as_scalars(a.table) + (int64_t)s * a.max_pages;
     int t0 = split * wk.chunk + wave * TOK;
-    int now[TILES], next[TILES];
-    auto pages_at = [&](int t, int* pages) {                  // behind the end any page will do: its tokens are not live
+    int pages[4][TILES];                                      // of this step and the three after it
+    auto pages_at = [&](int t, int* to) {                     // behind the end any page will do: its tokens are not live
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) pages[i] = table[(t + 16 * i < room ? t + 16 * i : room - 1) >> wk.log2_page];
+        for (int i = 0; i < TILES; ++i) to[i] = table[(t + 16 * i < room ? t + 16 * i : room - 1) >> wk.log2_page];
     };
-    pages_at(t0, now);
-    pages_at(t0 + STEP, next);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) pages_at(t0 + i * STEP, pages[i]);
     int len = as_scalars(a.lengths)[s];
     // Query heads head0 .. head0 + nh - 1 of the call are columns of the products, zeros behind them.  A piece that would reach beyond a
     // row, of queries, keys or values, is the row's last one instead: what it repeats is zero among the queries, and of the values
@@ -157,7 +157,6 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     // up per load; as neighbouring lanes read them here, rows, they are 16 or fewer, and LDS turns them round.  Piece p of row r lies at
     // p ^ (r % 16) of its row there, so that the 16 rows of one read meet different banks.
     uint32_t kr[TILES][KU][4], vf[VT][NV][VW];
-    kv_sizes4 sz[TILES];
     uint32_t k_off[KU], v_off[4][NV];                         // bytes from the first row of a tile
     char* const keys = lds + wave * (TOK * PIECES * 16);
 #pragma unroll
@@ -175,34 +174,54 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     const uint32_t row_bytes = (uint32_t)(D * ES), P1 = (1u << wk.log2_page) - 1, page_bytes = (uint32_t)wk.n_heads * row_bytes << wk.log2_page;
     const char* const k0 = (const char*)kpool + ((uint64_t)h * row_bytes << wk.log2_page);
     const char* const v0 = (const char*)vpool + ((uint64_t)h * row_bytes << wk.log2_page);
+    auto held_at = [&](int page) { return (uint32_t)page < (uint32_t)wk.n_pages; };
+    // One bit for each token of a step that takes part.  With sizes, rows of the others are not read: the request goes to the tile's
+    // first bytes instead (a prompt pruned in place may have nine such tokens in ten).
+    constexpr uint32_t ALL = BF ? 0xffffffffu : 0xffffu;
+    auto live_at = [&](int t, const int* pg, int size) -> uint32_t {
+        const int n = end - t;
+        uint32_t m = n >= TOK ? ALL : n > 0 ? (1u << n) - 1u : 0u;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) m &= held_at(pg[i]) ? ALL : ~(0xffffu << (16 * i));
+        if constexpr (SIZED) m &= (uint32_t)__ballot(size >= 1);
+        return m;
+    };
+    auto ask_size = [&](int t, const int* pg) -> int {        // of token `lane` of a step
+        if constexpr (!SIZED) return 1;
+        const int i = BF && (lane & 16) ? 1 : 0, page = BF && i ? pg[TILES - 1] : pg[0];
+        const uint32_t p = held_at(page) ? page : 0;
+        return wk.sizes[((uint64_t)p << wk.log2_page) + ((uint32_t)(t + 16 * i) & P1) + (lane & 15)];
+    };
     uint64_t tile[TILES];                                     // bytes to the tiles of the step that is asked for
-    auto ask_keys = [&](int t, const int* pages) {
+    auto ask_keys = [&](int t, const int* pg, uint32_t live) {
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {                     // without a page, page 0: its tokens are then not live
-            const uint32_t p = (uint32_t)pages[i] < (uint32_t)wk.n_pages ? pages[i] : 0, r = (uint32_t)(t + 16 * i) & P1;
+            const uint32_t p = held_at(pg[i]) ? pg[i] : 0, r = (uint32_t)(t + 16 * i) & P1;
             tile[i] = (uint64_t)p * page_bytes + r * row_bytes;
 #pragma unroll
-            for (int u = 0; u < KU; ++u) load_words<T, 4, SMALL>(kr[i][u], k0 + tile[i], k_off[u], ((lane % PIECES) ^ (((64 * u + lane) / PIECES) & SWZ)) * KE, D);
-        }
-    };
-    auto ask_values = [&](int t, const int* pages) {
-        if constexpr (SIZED) {
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) {
-                const uint32_t p = (uint32_t)pages[i] < (uint32_t)wk.n_pages ? pages[i] : 0;
-                sz[i] = *(const kv_sizes4*)((const char*)(wk.sizes + (((uint64_t)p << wk.log2_page) + ((uint32_t)(t + 16 * i) & P1))) + 16u * g);
+            for (int u = 0; u < KU; ++u) {
+                uint32_t off = k_off[u];
+                if constexpr (SIZED) off &= (uint32_t)__builtin_amdgcn_sbfe((int)(live >> (16 * i + 64 * u / PIECES)), lane / PIECES, 1);
+                load_words<T, 4, SMALL>(kr[i][u], k0 + tile[i], off, ((lane % PIECES) ^ (((64 * u + lane) / PIECES) & SWZ)) * KE, D);
             }
         }
+    };
+    auto ask_values = [&](uint32_t live) {
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t on = SIZED ? (uint32_t)__builtin_amdgcn_sbfe((int)(live >> (16 * i + j)), 4 * g, 1) : ~0u;
 #pragma unroll
-                for (int n = 0; n < NV; ++n) load_words<T, VW, SMALL>(vf[4 * i + j][n], v0 + tile[i], v_off[j][n], (16 * n + c) * VL, D);
+                for (int n = 0; n < NV; ++n) load_words<T, VW, SMALL>(vf[4 * i + j][n], v0 + tile[i], SIZED ? v_off[j][n] & on : v_off[j][n], (16 * n + c) * VL, D);
+            }
     };
+    int size = 1, size_next = 1;
     if (t0 < end) {
-        ask_keys(t0, now);
-        ask_values(t0, now);
+        size = ask_size(t0, pages[0]);
+        size_next = ask_size(t0 + STEP, pages[1]);
+        ask_keys(t0, pages[0], ~0u);
+        ask_values(~0u);
     }
     __syncthreads();                                          // the queries are in LDS
     uint32_t qf[NK][4];
@@ -215,6 +234,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 
     kv_f32x4 o[NV * VL] = {};
     float m = kLowest, l = 0.f, ls = 0.f;
+    uint32_t live = live_at(t0, pages[0], size);
     // MORE: the next step's keys take the place of this one's while the weights are formed, its values that of the values after them.
     // A step without a successor is code of its own: with the requests behind a condition, the wait for the values would have to be one
     // for everything in flight.
@@ -243,34 +263,19 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[4 * i + e] = z[e];
         }
-        bool whole = !SIZED && t0 + TOK <= end;
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) whole = whole && (uint32_t)now[i] < (uint32_t)wk.n_pages;
-        uint32_t live = 0;                                    // a bit for each of the lane's tokens
-        float lg[VT] = {};
-        if (!whole) {
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) {
-                const int n = (uint32_t)now[i] < (uint32_t)wk.n_pages ? end - (t0 + 16 * i + 4 * g) : 0;
-                live |= (n >= 4 ? 15u : n > 0 ? (1u << n) - 1u : 0u) << (4 * i);
-                if constexpr (SIZED) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (sz[i][e] < 1) live &= ~(1u << (4 * i + e));
-                        if (a.enhance) lg[4 * i + e] = __log2f((float)(sz[i][e] < 1 ? 1 : sz[i][e]));
-                    }
-                }
-            }
-            whole = __all(live == (1u << VT) - 1u);
-        }
-        int after[TILES];
+        uint32_t live_next = 0;
+        int size_after = 1;
         if constexpr (MORE) {
-            pages_at(t0 + 2 * STEP, after);
-            ask_keys(t0 + STEP, next);
+            live_next = live_at(t0 + STEP, pages[1], size_next);
+            pages_at(t0 + 3 * STEP, pages[3]);
+            size_after = ask_size(t0 + 2 * STEP, pages[2]);
+            ask_keys(t0 + STEP, pages[1], live_next);
         }
-        if (!whole) {
+        const uint32_t mine = live >> (4 * g);                // bits 0 .. 3, 16 .. 19: the lane's tokens
+        auto on = [&](int j) { return mine >> (j % 4 + 16 * (j / 4)) & 1; };
+        if (live != ALL) {
 #pragma unroll
-            for (int j = 0; j < VT; ++j) p[j] = live >> j & 1 ? p[j] : -__builtin_inff();
+            for (int j = 0; j < VT; ++j) p[j] = on(j) ? p[j] : -__builtin_inff();
         }
         float top = p[0];
 #pragma unroll
@@ -292,17 +297,18 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], wk.scale, -m));
             l += p[j];
         }
-        if constexpr (SIZED) {
+        if (SIZED && a.enhance) {
+            const float lg = __log2f((float)(size < 1 ? 1 : size));
 #pragma unroll
-            for (int j = 0; j < VT; ++j) ls += p[j] * lg[j];
+            for (int j = 0; j < VT; ++j) ls += p[j] * __shfl(lg, 4 * g + j % 4 + 16 * (j / 4), kWave);
         }
-        if (!whole) {
+        if (live != ALL) {
 #pragma unroll
             for (int j = 0; j < VT; ++j)
 #pragma unroll
                 for (int n = 0; n < NV; ++n)
 #pragma unroll
-                    for (int w = 0; w < VW; ++w) vf[j][n][w] = live >> j & 1 ? vf[j][n][w] : 0u;
+                    for (int w = 0; w < VW; ++w) vf[j][n][w] = on(j) ? vf[j][n][w] : 0u;
         }
         if constexpr (BF) {
             kv_bf16x8 hi, lo;
@@ -332,9 +338,12 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                         o[n * VL + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[j][n][e]), p[j], o[n * VL + e], 0, 0, 0);
         }
         if constexpr (MORE) {
-            ask_values(t0 + STEP, next);
+            ask_values(live_next);
+            live = live_next;
+            size = size_next;
+            size_next = size_after;
 #pragma unroll
-            for (int i = 0; i < TILES; ++i) { now[i] = next[i]; next[i] = after[i]; }
+            for (int i = 0; i < TILES; ++i) { pages[1][i] = pages[2][i]; pages[2][i] = pages[3][i]; }
         }
     };
     for (; t0 + STEP < end; t0 += STEP) step(std::true_type{});
@@ -484,23 +493,27 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     }
 }
 
-// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  Joining runs costs 4 us
-// behind the last one and 0.6 for every further trip to memory of the join; a workgroup that is alone on its unit takes a step in
-// 1.2 us as long as memory keeps up with all of them, which it does to 5.9 TB/s (all measured: 1 x 32768 tokens, 8 heads of 128, bf16,
-// 256 steps: 45.8 us with 32 steps to a workgroup, 30.5 with 16, 29.5 with 12, 30.8 with 8, 35.2 with 4, 61 with 2).  At most 8 (1024
-// tokens in bf16) where that leaves two workgroups to a unit: `all` is a bound, and one sequence of that length among short
-// ones would be waited for (64 sequences of 1 to 8200 tokens: 86 us with 16 steps, 76 with 8; 64 of 4096 lose 193 for 180).
-int attend_steps(int64_t tiles, int all, int quads, double step_bytes)
+// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  All measured:
+// memory keeps up with 5.9 TB/s of steps, less a share for the parts of runs that are joined and for workgroups that come and go; a
+// workgroup that is alone on its unit takes a step of 64 KB in 1.4 us; runs arrive at a word one every third of a microsecond; the join takes
+// 4 us and 0.6 more for every further trip to memory (1 x 32768 tokens, 8 heads of 128, bf16, 256 steps: 45.8 us with 32 steps to a
+// workgroup, 30.0 with 16, 28.3 with 12, 28.9 with 8, 31.3 with 4, 48 with 2, 91 with 1; 8 x 1100, 4 heads, 9 steps: 10.4 with
+// 1, 9.7 with 2, 10.5 with 4, 11.2 with 9).  At most 8 (1024 tokens in bf16) where that leaves two workgroups to a unit: `all` is
+// a bound, and one sequence of that length among short ones would be waited for (64 sequences of 1 to 8200 tokens, 8 heads: 86 us with 16
+// steps, 75 with 8; 64 of 4096 lose 194 for 180).
+int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes, int resident)
 {
-    const int64_t fewest = std::max<int64_t>((all + kMaxSplits - 1) / kMaxSplits, (tiles * all >> 22) + 1);
-    const int64_t most = tiles * ((all + 7) / 8) >= 512 ? 8 : all;
+    const int64_t fewest = std::max<int64_t>((all + kMaxSplits - 1) / kMaxSplits, (rows * tiles * all >> 22) + 1);
+    const int64_t most = rows * tiles * ((all + 7) / 8) >= 512 ? 8 : all;
     const int groups = quads < kWaves * 64 ? kWaves * 64 / quads : 1;
-    const double memory = (double)tiles * all * step_bytes / 5.9e6;
+    const double step_us = std::max(0.5, step_bytes / 65536.0);
     int64_t best = std::min<int64_t>(fewest, all);
     double least = 1e300;
     for (int64_t n = best; n <= std::min<int64_t>(most, all); n += n < 4 ? 1 : n / 4) {
-        const int64_t runs = (all + n - 1) / n, each = (tiles * runs + 255) / 256;
-        const double us = std::max(memory, n * (0.8 + 0.4 * each)) + (runs > 1 ? 4.0 + 0.6 * ((runs - 1) / (16 * groups)) : 0.0);
+        const int64_t runs = (all + n - 1) / n, each = (rows * tiles * runs + 255) / 256;
+        const double memory = (double)rows * all * step_bytes / 5.9e6, steps = n * step_us * (resident > 1 ? 1.0 + 0.4 * (double)each : 1.4 * (double)each);
+        const double us = runs == 1 ? std::max(memory, steps)
+                                    : std::max({memory * (1.0 + 0.25 / std::sqrt((double)n)), steps, 0.33 * (double)runs}) + 4.0 + 0.6 * (double)((runs - 1) / (16 * groups));
         if (us < least) { least = us; best = n; }
     }
     return (int)best;
@@ -522,7 +535,7 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
     const int waves = kWaves, step = waves * (dt == LUVC_F32 ? 16 : 32);
-    p.chunk = attend_steps(p.rows * p.tiles, (max_tokens + step - 1) / step, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
+    p.chunk = attend_steps(p.rows, p.tiles, (max_tokens + step - 1) / step, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2) * step;
     p.splits = (max_tokens + p.chunk - 1) / p.chunk;
     p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
