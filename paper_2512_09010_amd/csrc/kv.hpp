@@ -10,14 +10,6 @@ inline size_t kv_esize(const luvc_kv_cache& c) { return c.dtype == LUVC_F32 ? 4 
 inline int64_t kv_page_elems(const luvc_kv_cache& c) { return (int64_t)c.n_heads * c.page_tokens * c.D; }
 inline int kv_log2_page(const luvc_kv_cache& c) { return 31 - __builtin_clz((unsigned)c.page_tokens); }
 
-// Quotients by a number that the host knows, as a product: exact for n < 2^26 and d <= 2^6, or n * d < 2^32
-struct KvDiv {
-    uint64_t m;
-    uint32_t d;
-};
-inline KvDiv kv_div(uint32_t d) { return KvDiv{((1ull << 32) + d - 1) / d, d}; }
-__device__ __forceinline__ uint32_t operator/(uint32_t n, const KvDiv& d) { return (uint32_t)((n * d.m) >> 32); }
-
 // Bytes that rows may be moved in at a time: the largest power of two up to 16 that divides everything in `bits` (offsets, lengths and
 // addresses in bytes, or'ed)
 inline int kv_piece(uint64_t bits)
