@@ -383,7 +383,7 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
  * and the output is rounded once.  The parts of a long sequence are joined in a fixed order: same input, same bits.
  * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype); any contents, one per call
  * in flight, also for calls in captured graphs.
- * Limits: n_seqs * n_q_heads < 2^24, max_tokens < 2^30.
+ * Limits: n_seqs * n_q_heads < 2^22, max_tokens < 2^30.
  */
 size_t luvc_kv_attend_workspace_bytes(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens);
 luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q, int64_t q_stride, int n_q_heads, int n_seqs,
@@ -403,7 +403,7 @@ luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q,
  * Pages of table_out must not be read by the call (from any of its sequences), with one exception: a page of tokens that stay
  * where they are, so that first[i] / page_tokens pages of either table's row may be the same.
  * The host arrays are used up when the call returns.  A call of more than 64 sequences is several launches.
- * Limits: sequences of fewer than 2^29 tokens.
+ * Limits: sequences of fewer than 2^25 tokens.
  */
 luvc_status luvc_kv_compact(const luvc_kv_cache* cache, int n_seqs, const int32_t* lengths, const int32_t* first, const int32_t* span,
                             const int32_t* n_keep, const int32_t* kept_idx, const int32_t* table_in, int max_pages_in,

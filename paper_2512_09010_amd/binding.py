@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from itertools import chain
 from typing import List, Optional, Sequence, Tuple
 
@@ -606,36 +607,45 @@ class KvCache:
 
 def _here(nat, cache, *tensors):
     """The library launches on the current GPU: its streams do not reach another one's memory."""
-    assert cache.index == nat.device(), "the cache is not on the current device"
+    index = cache.index
+    assert index == nat.device(), "the cache is not on the current device"
     for t in tensors:
-        assert t is None or t.get_device() == cache.index, "a tensor is not on the cache's device"
+        assert t is None or t.get_device() == index, "a tensor is not on the cache's device"
 
 
 def _host_ints(values):
-    """(what keeps them alive, address, count) of int32 on the host: a contiguous CPU tensor or array of them as it is, anything else copied."""
-    torch = _native().torch
-    if isinstance(values, torch.Tensor) and values.dtype == torch.int32 and not values.is_cuda and values.is_contiguous():
-        return values, values.data_ptr(), values.numel()
-    if isinstance(values, torch.Tensor):
+    """(what keeps them alive, address, count) of int32 on the host: a contiguous CPU tensor of them as it is, anything else copied."""
+    nat = _native()
+    if isinstance(values, nat.torch.Tensor):
+        if values.dtype is nat.i32 and not values.is_cuda and values.is_contiguous():
+            return values, values.data_ptr(), values.numel()
         values = values.flatten().tolist()
-    arr = _i32(list(values))
-    return arr, ctypes.addressof(arr), len(values)
+    arr = array("i", values)
+    return arr, arr.buffer_info()[0], len(arr)
+
+
+def _rows(t, T, H, D):
+    """Elements between the tokens of t [T, H, D], whose heads lie one after the other."""
+    st, sh, sd = t.stride()
+    assert (sd == 1 or D == 1) and (sh == D or H == 1), "the heads of a token must be dense"
+    return st if T > 1 else H * D
 
 
 def luvc_kv_write(cache: KvCache, layer: int, k, v, pos, table, seq=None, sizes=None, stream=None):
     """k, v [T, n_heads, D] (dense heads, tokens evenly strided) go to positions pos [T] of the table rows seq [T] (None: token t is of
     row t); table int32 [n_seqs, max_pages]."""
     nat = _native()
-    T, H, D = k.shape
-    assert v.shape == k.shape and (H, D) == (cache.n_heads, cache.D) and k.dtype == cache.dtype and v.dtype == cache.dtype
-    assert T == 0 or ((D == 1 or k.stride(2) == v.stride(2) == 1) and (H == 1 or k.stride(1) == v.stride(1) == D))
-    assert table.dim() == 2 and table.dtype == nat.i32 and table.is_contiguous()
+    shape, i32 = k.shape, nat.i32
+    T, H, D = shape
+    assert v.shape == shape and H == cache.n_heads and D == cache.D and k.dtype is cache.dtype and v.dtype is cache.dtype
+    n_seqs, width = table.shape
+    assert table.dtype is i32 and table.is_contiguous()
     _here(nat, cache, k, v, pos, table, seq, sizes)
-    for t in (pos, seq, sizes):
-        assert t is None or (t.dtype == nat.i32 and t.is_contiguous() and t.numel() == T)
-    ks, vs = (k.stride(0), v.stride(0)) if T > 1 else (H * D, H * D)
-    _check(nat.call(nat.luvc_kv_write, cache.addr, int(layer), k.data_ptr(), ks, v.data_ptr(), vs, _ptr(sizes), T, _ptr(seq), pos.data_ptr(),
-                    table.data_ptr(), table.shape[0], table.shape[1], nat.stream(stream)))
+    assert pos.dtype is i32 and pos.is_contiguous() and pos.numel() == T
+    assert seq is None or (seq.dtype is i32 and seq.is_contiguous() and seq.numel() == T)
+    assert sizes is None or (sizes.dtype is i32 and sizes.is_contiguous() and sizes.numel() == T)
+    _check(nat.call(nat.luvc_kv_write, cache.addr, int(layer), k.data_ptr(), _rows(k, T, H, D), v.data_ptr(), _rows(v, T, H, D), _ptr(sizes), T, _ptr(seq),
+                    pos.data_ptr(), table.data_ptr(), n_seqs, width, nat.stream(stream)))
 
 
 def luvc_kv_attend_workspace_bytes(cache: KvCache, n_seqs: int, n_q_heads: int, max_tokens: int) -> int:
@@ -648,24 +658,25 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
     tokens in the pages of table [n_seqs, max_pages].  max_tokens: no sequence is longer (None: what the table holds).
     Returns out [n_seqs, n_q_heads, D]."""
     nat = _native()
-    S, Hq, D = q.shape
-    assert D == cache.D and q.dtype == cache.dtype and (S == 0 or ((D == 1 or q.stride(2) == 1) and (Hq == 1 or q.stride(1) == D)))
-    assert table.dim() == 2 and table.shape[0] == S and table.dtype == nat.i32 and table.is_contiguous()
-    assert lengths.dtype == nat.i32 and lengths.is_contiguous() and lengths.numel() == S
+    shape, i32, dtype = q.shape, nat.i32, cache.dtype
+    S, Hq, D = shape
+    n_seqs, width = table.shape
+    assert D == cache.D and q.dtype is dtype
+    assert n_seqs == S and table.dtype is i32 and table.is_contiguous()
+    assert lengths.dtype is i32 and lengths.is_contiguous() and lengths.numel() == S
     if max_tokens is None:
-        max_tokens = min(max(table.shape[1] * cache.page_tokens, 1), (1 << 30) - 1)
+        max_tokens = min(max(width * cache.page_tokens, 1), (1 << 30) - 1)
     if workspace is None:
         need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
         workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
     if out is None:
-        out = nat.torch.empty((S, Hq, D), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and (S == 0 or ((D == 1 or out.stride(2) == 1) and (Hq == 1 or out.stride(1) == D)))
+        out = nat.torch.empty(shape, dtype=dtype, device=q.device)
+    assert out.shape == shape and out.dtype is dtype
     _here(nat, cache, q, table, lengths, workspace, out)
-    qs, os = (q.stride(0), out.stride(0)) if S > 1 else (Hq * D, Hq * D)
     sc = None if scale is None else ctypes.c_double(scale)
-    _check(nat.call(nat.luvc_kv_attend, cache.addr, int(layer), q.data_ptr(), qs, Hq, S, table.data_ptr(), table.shape[1], lengths.data_ptr(),
-                    int(max_tokens), None if sc is None else ctypes.addressof(sc), int(bool(enhance)), out.data_ptr(), os,
-                    workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
+    _check(nat.call(nat.luvc_kv_attend, cache.addr, int(layer), q.data_ptr(), _rows(q, S, Hq, D), Hq, S, table.data_ptr(), width, lengths.data_ptr(),
+                    int(max_tokens), None if sc is None else ctypes.addressof(sc), int(bool(enhance)), out.data_ptr(), _rows(out, S, Hq, D),
+                    workspace.data_ptr(), workspace.nbytes, nat.stream(stream)))
     return out
 
 
@@ -673,17 +684,18 @@ def luvc_kv_compact(cache: KvCache, kept_idx, lengths, first, span, n_keep, tabl
     """Of sequence i with lengths[i] tokens (host integers, as first, span and n_keep) the span[i] visual ones from first[i] on shrink to the
     n_keep[i] listed in kept_idx (CUDA int32, sequence after sequence).  Returns the lengths afterwards."""
     nat = _native()
-    S = len(lengths)
-    assert len(first) == len(span) == len(n_keep) == S
-    for t in (table_in, table_out):
-        assert t.dim() == 2 and t.shape[0] == S and t.dtype == nat.i32 and t.is_contiguous()
+    (n, n_at, S), (f, f_at, S1), (w, w_at, S2), (k, k_at, S3) = _host_ints(lengths), _host_ints(first), _host_ints(span), _host_ints(n_keep)
+    assert S == S1 == S2 == S3
+    (rows_in, width_in), (rows_out, width_out) = table_in.shape, table_out.shape
+    assert rows_in == rows_out == S
     _here(nat, cache, kept_idx, table_in, table_out)
-    arrays = [_host_ints(v) for v in (lengths, first, span, n_keep)]
-    after = [int(a) - int(b) + int(c) for a, b, c in zip(lengths, span, n_keep)]
-    assert kept_idx is None or (kept_idx.dtype == nat.i32 and kept_idx.is_contiguous() and kept_idx.numel() == sum(int(c) for c in n_keep))
-    _check(nat.call(nat.luvc_kv_compact, cache.addr, S, *(a[1] for a in arrays), _ptr(kept_idx), table_in.data_ptr(), table_in.shape[1],
-                    table_out.data_ptr(), table_out.shape[1], nat.stream(stream)))
-    return after
+    for t in (kept_idx, table_in, table_out):
+        assert t is None or (t.dtype is nat.i32 and t.is_contiguous())
+    before, spans, keeps = n.tolist(), w.tolist(), k.tolist()
+    assert kept_idx is None or kept_idx.numel() == sum(keeps)
+    _check(nat.call(nat.luvc_kv_compact, cache.addr, S, n_at, f_at, w_at, k_at, _ptr(kept_idx), table_in.data_ptr(), width_in, table_out.data_ptr(),
+                    width_out, nat.stream(stream)))
+    return [a - b + c for a, b, c in zip(before, spans, keeps)]
 
 
 def luvc_kv_copy_pages(cache: KvCache, src, dst, stream=None):
@@ -695,9 +707,8 @@ def luvc_kv_copy_pages(cache: KvCache, src, dst, stream=None):
     _check(nat.call(nat.luvc_kv_copy_pages, cache.addr, src_at, dst_at, n, nat.stream(stream)))
 
 
-def _refs(refs):
-    torch = _native().torch
-    assert isinstance(refs, torch.Tensor) and refs.dtype == torch.int32 and not refs.is_cuda and refs.is_contiguous()
+def _refs(nat, refs):
+    assert isinstance(refs, nat.torch.Tensor) and refs.dtype is nat.i32 and not refs.is_cuda and refs.is_contiguous()
     return refs.data_ptr()
 
 
@@ -705,7 +716,7 @@ def luvc_kv_take(refs, n: int):
     """The n lowest pages that refs (CPU int32 [n_pages], changed in place) counts 0; they count 1 then.  Returns them, CPU int32 [n]."""
     nat = _native()
     pages = nat.torch.empty((max(int(n), 0),), dtype=nat.i32)
-    _check(nat.call(nat.luvc_kv_take, _refs(refs), refs.numel(), int(n), pages.data_ptr() if n > 0 else None))
+    _check(nat.call(nat.luvc_kv_take, _refs(nat, refs), refs.numel(), int(n), pages.data_ptr() if n > 0 else None))
     return pages
 
 
@@ -714,12 +725,11 @@ def luvc_kv_fork(cache: KvCache, refs, pages, length: int, n_children: int, stre
     [n_children, ceil(length / page_tokens)]."""
     nat = _native()
     _here(nat, cache)
-    assert refs.numel() == cache.n_pages
     a, at, n = _host_ints(pages)
     used = -(-int(length) // cache.page_tokens)
-    assert n >= used
+    assert n >= used and refs.numel() == cache.n_pages
     children = nat.torch.empty((max(int(n_children), 0), max(used, 0)), dtype=nat.i32)
-    _check(nat.call(nat.luvc_kv_fork, cache.addr, _refs(refs), at, int(length), int(n_children), children.data_ptr(), nat.stream(stream)))
+    _check(nat.call(nat.luvc_kv_fork, cache.addr, _refs(nat, refs), at, int(length), int(n_children), children.data_ptr(), nat.stream(stream)))
     return children
 
 
@@ -727,7 +737,7 @@ def luvc_kv_release(refs, pages):
     """Every page of `pages` (host integers) counts one less in refs (CPU int32 [n_pages], changed in place)."""
     nat = _native()
     a, at, n = _host_ints(pages)
-    _check(nat.call(nat.luvc_kv_release, _refs(refs), refs.numel(), at, n))
+    _check(nat.call(nat.luvc_kv_release, _refs(nat, refs), refs.numel(), at, n))
 
 
 class LaunchProfile:

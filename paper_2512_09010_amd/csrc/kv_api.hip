@@ -91,7 +91,7 @@ static bool attend_sizes_ok(const luvc_kv_cache* cache, int n_seqs, int n_q_head
     if (n_seqs < 1 || n_q_heads < 1 || max_tokens < 1) { set_error("n_seqs, n_q_heads and max_tokens must be positive (got %d, %d, %d)", n_seqs, n_q_heads, max_tokens); return false; }
     if (n_q_heads % cache->n_heads) { set_error("n_q_heads=%d is no multiple of the cache's %d heads", n_q_heads, cache->n_heads); return false; }
     if (max_tokens >= (1 << 30)) { set_error("max_tokens must stay below 2^30"); return false; }
-    if ((int64_t)n_seqs * n_q_heads >= ((int64_t)1 << 24)) { set_error("n_seqs * n_q_heads must stay below 2^24"); return false; }
+    if ((int64_t)n_seqs * n_q_heads >= ((int64_t)1 << 22)) { set_error("n_seqs * n_q_heads must stay below 2^22"); return false; }
     return true;
 }
 
@@ -115,11 +115,11 @@ luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q,
     if (q_stride < row || out_stride < row) { set_error("sequence strides must be at least n_q_heads * D = %lld", (long long)row); return LUVC_ERR_INVALID_ARG; }
     if (((uintptr_t)q | (uintptr_t)out) % kv_esize(*cache)) { set_error("q and out must be aligned to their elements"); return LUVC_ERR_INVALID_ARG; }
     if (enhance && !cache->sizes) { set_error("the term log s needs a cache with sizes"); return LUVC_ERR_INVALID_ARG; }
-    const double sc = scale ? *scale : 1.0 / std::sqrt((double)cache->D);
-    if (!std::isfinite(sc)) { set_error("scale must be finite"); return LUVC_ERR_INVALID_ARG; }
+    const float sc = (float)(scale ? *scale : 1.0 / std::sqrt((double)cache->D));
+    if (!std::isfinite(sc)) { set_error("scale must be finite in fp32"); return LUVC_ERR_INVALID_ARG; }
     const size_t need = kv_attend_workspace(n_seqs, n_q_heads, cache->n_heads, cache->D, cache->dtype, max_tokens);
     if (!workspace_ok(workspace, workspace_bytes, need)) return LUVC_ERR_WORKSPACE;
-    const KvAttend a{q, out, q_stride, out_stride, table, lengths, n_seqs, n_q_heads, max_pages, max_tokens, (float)sc, enhance != 0};
+    const KvAttend a{q, out, q_stride, out_stride, table, lengths, n_seqs, n_q_heads, max_pages, max_tokens, sc, enhance != 0};
     return kv_attend_run(*cache, layer, a, workspace, (hipStream_t)hip_stream);
 }
 
@@ -146,7 +146,7 @@ luvc_status luvc_kv_compact(const luvc_kv_cache* cache, int n_seqs, const int32_
             set_error("sequence %d: %d tokens before and %lld after do not fit the tables' %d and %d pages", i, lengths[i], (long long)after, max_pages_in, max_pages_out);
             return LUVC_ERR_INVALID_ARG;
         }
-        if (lengths[i] >= (1 << 29)) { set_error("sequence %d: lengths must stay below 2^29", i); return LUVC_ERR_UNSUPPORTED; }
+        if (lengths[i] >= (1 << 25)) { set_error("sequence %d: lengths must stay below 2^25", i); return LUVC_ERR_UNSUPPORTED; }
         kept += n_keep[i];
     }
     if (kept && !kept_idx) { set_error("kept_idx must not be NULL"); return LUVC_ERR_INVALID_ARG; }
