@@ -46,7 +46,7 @@ constexpr int kMaxSplits = 256;
 constexpr float kLogE = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kMoreWaves = 8;
 
 __device__ __forceinline__ float xor16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32, kWave); }
@@ -85,13 +85,13 @@ struct KvWork {
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
 
-// DP: channels with room (64, 128, 256); SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
-template <typename T, int DP, bool SMALL, bool SIZED>
-__global__ void __launch_bounds__(kWaves * 64, DP == 256 ? 1 : DP == 64 ? 4 : sizeof(T) == 4 ? 2 : 3)
+// DP: channels with room (64, 128, 256); NW: wavefronts; SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
+template <typename T, int DP, int NW, bool SMALL, bool SIZED>
+__global__ void __launch_bounds__(NW * 64, DP == 256 ? 1 : DP == 64 ? 4 : sizeof(T) == 4 || NW == kMoreWaves ? 2 : 3)
 kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, KvAttend a)
 {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int ES = (int)sizeof(T), NW = kWaves, NT = NW * 64;
+    constexpr int ES = (int)sizeof(T), NT = NW * 64;
     constexpr int TILES = BF ? 2 : 1, TOK = 16 * TILES, STEP = NW * TOK;      // tokens of a wavefront's step, of the workgroup's
     constexpr int KE = 16 / ES;                               // elements in 16 bytes
     constexpr int NK = DP / (4 * KE);                         // pieces of a key per lane
@@ -99,7 +99,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     constexpr int VT = 4 * TILES;                             // tokens of a lane's part of the second sum
     constexpr int LD = DP + 4, PIECES = DP / KE;              // a row of outputs in LDS; pieces of a query or a key
     constexpr int KU = PIECES / 4, SWZ = PIECES < 16 ? PIECES - 1 : 15;       // loads of a tile of keys, 64 pieces each
-    // In LDS, one after the other: the wavefronts' keys, queries; then parts of the outputs; then weights and partial sums of the join
+    // In LDS, one after the other: the wavefronts' keys, queries; then parts of the outputs; then partial sums of the join
     extern __shared__ __align__(16) char lds[];
     float(*sm)[16] = (float(*)[16])(lds + wk.lds_words), (*sl)[16] = sm + NW;
     int& last_flag = *(int*)(sl + NW);
@@ -363,25 +363,25 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int d = (16 * n + 4 * g + i) * VL;
-                d = SMALL || d < D - VL ? d : D - VL;
-                if (SMALL && d >= D) continue;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < VL; e += 4) {
-                    kv_f32x4u w;
+                    kv_f32x4 w;
 #pragma unroll
                     for (int b = 0; b < 4; ++b) w[b] = o[n * VL + e + b][i] + ls;
-                    *(kv_f32x4u*)&so[(wave * wk.cols + c) * LD + d + e] = w;
+                    *(kv_f32x4*)&so[(wave * wk.cols + c) * LD + (16 * n + 4 * g + i) * VL + e] = w;
                 }
-            }
     }
     if (splits > 1 && tid == 0 && (seen >> 16) != wk.tag) {
         tile_tag_t expect = seen;
         (void)__hip_atomic_compare_exchange_strong(word, &expect, wk.tag << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
-    const int quads = (D + 3) / 4, items = nh * quads, part = wk.cols * wk.parts_row;
+    // Four channels of a head to a thread, in the order of heads of DP channels; further rows of threads, where heads are few, share runs
+    constexpr int QUADS = DP / 4;
+    const int log2_items = 31 - __builtin_clz(QUADS) + (nh > 1 ? 32 - __builtin_clz(nh - 1) : 0), part = wk.cols * wk.parts_row;
+    const int groups = (1 << log2_items) < NT ? NT >> log2_items : 1, grp = groups > 1 ? tid >> log2_items : 0;
+    const int item0 = groups > 1 ? tid & ((1 << log2_items) - 1) : tid;
     float* parts = wk.parts + ((int64_t)row * wk.tiles + qt) * wk.splits * part;
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, splits * part * 4, 0x00020000);
     auto store = [&](int col, int d, kv_f32x4 v) {
@@ -402,27 +402,42 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             }
         }
     };
-    for (int i = tid; i < items; i += NT) {
-        const int col = i / quads, d = i % quads * 4;
-        float top = sm[0][col];
+    // channels d .. d + 3 of a wavefront's part: the piece that would reach beyond the row holds the row's last channels
+    const int even = SMALL ? DP : D / VL * VL;
+    auto part_of = [&](const float* row_part, int d) {
+        if (d + 4 <= even) return *(const kv_f32x4*)(row_part + d);
+        kv_f32x4 v;
 #pragma unroll
-        for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w][col]);
-        float sum = 0.f;
-        kv_f32x4 v = {};
+        for (int b = 0; b < 4; ++b) v[b] = row_part[d + b < even ? d + b : d + b < D ? d + b + VL - (D - even) : 0];
+        return v;
+    };
+    struct Sum {                                              // weighted values, their weights' sum, and the maximum both refer to
+        float top, sum;
+        kv_f32x4 v;
+        __device__ __forceinline__ void add(float m, float l, kv_f32x4 x)
+        {
+            const float t = fmaxf(top, m), f = __builtin_amdgcn_exp2f(top - t), w = __builtin_amdgcn_exp2f(m - t);
+            top = t;
+            sum = sum * f + l * w;
+            v = v * f + x * w;
+        }
+        __device__ __forceinline__ kv_f32x4 mean() const { return v * (sum > 0.f ? 1.f / sum : 0.f); }
+    };
+    if (grp == 0)
+        for (int i = item0; i < nh * QUADS; i += NT) {
+            const int col = i / QUADS, d = i % QUADS * 4;
+            if (d >= D) continue;
+            Sum t{sm[0][col], sl[0][col], part_of(&so[col * LD], d)};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm[w][col] - top);
-            sum += f * sl[w][col];
-            v += f * *(const kv_f32x4*)&so[(w * wk.cols + col) * LD + d];
+            for (int w = 1; w < NW; ++w) t.add(sm[w][col], sl[w][col], part_of(&so[(w * wk.cols + col) * LD], d));
+            if (splits == 1) {
+                store(col, d, t.mean());
+            } else {
+                const uint32_t at = (uint32_t)((split * part + col * wk.parts_row) * 4);
+                tile_vec<4>::store(__builtin_bit_cast(tile_vec<4>::type, t.v), all, at + d * 4);
+                if (d == 0) tile_vec<2>::store(tile_vec<2>::type{__float_as_uint(t.top), __float_as_uint(t.sum)}, all, at + (wk.parts_row - 4) * 4);
+            }
         }
-        if (splits == 1) {
-            store(col, d, v * (sum > 0.f ? 1.f / sum : 0.f));
-        } else {
-            tile_vec<4>::store(__builtin_bit_cast(tile_vec<4>::type, v), all, (uint32_t)((split * part + col * wk.parts_row + d) * 4));
-            if (d == 0)
-                tile_vec<4>::store(tile_vec<4>::type{__float_as_uint(top), __float_as_uint(sum), 0u, 0u}, all, (uint32_t)((split * part + (col + 1) * wk.parts_row - 4) * 4));
-        }
-    }
     if (splits == 1) return;
 
     // ---- the runs of the sequence, by the workgroup that ends last
@@ -435,62 +450,42 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     }
     __syncthreads();
     if (!last_flag) return;
-    float *weight = so, *total = sl[0], *red = so + kMaxSplits * 16;      // [splits][16], [cols], [NT][4]
-    // Few channels in all: several threads to four of them, each with every groups-th run.  The first AHEAD runs of a thread are asked for
-    // together with the maxima and sums that their weights are formed of.
-    constexpr int AHEAD = 16;
-    const int groups = items < NT ? NT / items : 1;
-    const int item0 = groups > 1 ? tid % items : tid, grp = groups > 1 ? tid / items : 0;
-    for (int i0 = 0; i0 < items; i0 += NT) {
-        const int i = i0 + item0, col = i / quads, d = i % quads * 4;
-        const bool in = i < items && grp < groups;
-        kv_f32x4 v = {};
-        for (int k0 = 0; k0 < splits; k0 += AHEAD * groups) {
-            tile_vec<4>::type x[AHEAD];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int run = k0 + k * groups + grp;
-                x[k] = tile_vec<4>::load(all, (uint32_t)(((in && run < splits ? run : 0) * part + (in ? col * wk.parts_row + d : 0)) * 4));
-            }
-            if (i0 == 0 && k0 == 0) {
+    constexpr int AHEAD = 8;                                  // runs of a thread in flight
+    for (int i0 = 0; i0 < nh * QUADS; i0 += NT) {
+        const int i = i0 + item0, col = i / QUADS, d = i % QUADS * 4;
+        const bool in = col < nh && d < D;
+        const uint32_t at = in ? (uint32_t)(col * wk.parts_row * 4) : 0u;
+        Sum t{kLowest, 0.f, {}};
 #pragma unroll 1
-                for (int u = wave; u < nh; u += NW) {
-                    float mx[kMaxSplits / 64], sx[kMaxSplits / 64], top = kLowest, sum = 0.f;
+        for (int k0 = grp; k0 < splits; k0 += AHEAD * groups) {
+            tile_vec<4>::type x[AHEAD];
+            tile_vec<2>::type ml[AHEAD];
 #pragma unroll
-                    for (int k = 0; k < kMaxSplits / 64; ++k) {
-                        const int r = lane + 64 * k;
-                        const tile_vec<4>::type w = tile_vec<4>::load(all, (uint32_t)(((r < splits ? r : 0) * part + (u + 1) * wk.parts_row - 4) * 4));
-                        mx[k] = r < splits ? __uint_as_float(w[0]) : kLowest;
-                        sx[k] = r < splits ? __uint_as_float(w[1]) : 0.f;
-                        top = fmaxf(top, mx[k]);
-                    }
-#pragma unroll
-                    for (int b = 32; b > 0; b >>= 1) top = fmaxf(top, __shfl_xor(top, b, kWave));
-#pragma unroll
-                    for (int k = 0; k < kMaxSplits / 64; ++k) {
-                        const float f = __builtin_amdgcn_exp2f(mx[k] - top);
-                        sum += f * sx[k];
-                        if (lane + 64 * k < splits) weight[(lane + 64 * k) * 16 + u] = f;
-                    }
-                    sum = wave_sum(sum);
-                    if (lane == 0) total[u] = sum > 0.f ? 1.f / sum : 0.f;
-                }
-                __syncthreads();
+            for (int k = 0; k < AHEAD; ++k) {
+                const int run = k0 + k * groups;
+                const uint32_t from = (uint32_t)((run < splits ? run : splits - 1) * part * 4) + at;
+                x[k] = tile_vec<4>::load(all, from + (in ? d * 4 : 0));
+                ml[k] = tile_vec<2>::load(all, from + (wk.parts_row - 4) * 4);
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int run = k0 + k * groups + grp;
-                const float f = in && run < splits ? weight[run * 16 + col] : 0.f;
-                v += f * __builtin_bit_cast(kv_f32x4, x[k]);
+                const bool there = k0 + k * groups < splits;
+                t.add(there ? __uint_as_float(ml[k][0]) : kLowest, there ? __uint_as_float(ml[k][1]) : 0.f, there ? __builtin_bit_cast(kv_f32x4, x[k]) : kv_f32x4{});
             }
         }
-        if (groups > 1) {
-            *(kv_f32x4*)&red[tid * 4] = v;
+        if (groups > 1) {                                     // nh * QUADS < NT: one round
+            float* red = so + tid * 8;
+            *(kv_f32x4*)red = t.v;
+            red[4] = t.top;
+            red[5] = t.sum;
             __syncthreads();
-            if (in && grp == 0)
-                for (int k = 1; k < groups; ++k) v += *(const kv_f32x4*)&red[(k * items + i) * 4];
+#pragma unroll 1
+            for (int k = 1; grp == 0 && k < groups; ++k) {
+                red += 8 << log2_items;
+                t.add(red[4], red[5], *(const kv_f32x4*)red);
+            }
         }
-        if (in && grp == 0) store(col, d, v * total[col]);
+        if (in && grp == 0) store(col, d, t.mean());
     }
 }
 
@@ -522,7 +517,7 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes,
 
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, tiles, cols, chunk, splits, parts_row, lds_words;
+    int dp, waves, tiles, cols, chunk, splits, parts_row, lds_words;
     int64_t rows;
     unsigned blocks;
     size_t words, bytes, lds;
@@ -535,39 +530,49 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.tiles = (group + 15) / 16;
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
-    const int waves = kWaves, step = waves * (dt == LUVC_F32 ? 16 : 32);
-    p.chunk = attend_steps(p.rows, p.tiles, (max_tokens + step - 1) / step, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2) * step;
+    const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
+    // up to four steps of twice the wavefronts need no join, which is worth more than four steps take, where every workgroup has a unit
+    // of its own (1 x 208 tokens, 32 heads of 128, fp32: 9.4 us joined, JOINED)
+    p.waves = p.dp < 256 && all > 1 && all <= 8 && p.rows * p.tiles <= 256 ? kMoreWaves : kWaves;
+    p.chunk = (p.waves == kMoreWaves ? (all + 1) / 2 * 2 : attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2)) * step;
     p.splits = (max_tokens + p.chunk - 1) / p.chunk;
     p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
     p.words = align_up((size_t)p.rows * p.tiles * sizeof(tile_tag_t));
     p.bytes = p.words + (p.splits > 1 ? align_up((size_t)p.rows * p.tiles * p.splits * p.cols * p.parts_row * sizeof(float)) : 0);
-    // keys and queries; parts of the wavefronts; weights of the runs and partial sums over them.  Then maxima, sums, a word
-    const size_t front = (size_t)(waves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)waves * p.cols * (p.dp + 4) * sizeof(float);
-    const size_t join = p.splits > 1 ? (size_t)kMaxSplits * 16 * sizeof(float) + (size_t)waves * 64 * 16 : 0;
+    // keys and queries; parts of the wavefronts; partial sums over runs.  Then maxima, sums, a word
+    const size_t front = (size_t)(p.waves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)p.waves * p.cols * (p.dp + 4) * sizeof(float);
+    const size_t join = p.splits > 1 ? (size_t)p.waves * 64 * 8 * sizeof(float) : 0;
     size_t most = front > parts ? front : parts;
     most = most > join ? most : join;
     p.lds_words = (int)align_up(most, 16);
-    p.lds = p.lds_words + (2 * (size_t)waves * 16 + 4) * sizeof(float);
+    p.lds = p.lds_words + (2 * (size_t)p.waves * 16 + 4) * sizeof(float);
     return p;
 }
 
-template <typename T, int DP, bool SMALL>
+template <typename T, int DP, int NW, bool SMALL>
 void attend_launch(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
     const T *k = (const T*)c.k + layer * c.layer_stride, *v = (const T*)c.v + layer * c.layer_stride;
-    const dim3 grid(p.blocks), block(kWaves * 64);
-    if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
-    else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
+    const dim3 grid(p.blocks), block(NW * 64);
+    if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, NW, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
+    else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, NW, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
+}
+
+template <typename T, int DP, bool SMALL>
+void attend_waves(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
+{
+    if (p.waves == kMoreWaves) attend_launch<T, DP, kMoreWaves, SMALL>(p, c, layer, wk, a, st);
+    else attend_launch<T, DP, kWaves, SMALL>(p, c, layer, wk, a, st);
 }
 
 template <typename T>
 void attend_shape(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
-    if (c.D * sizeof(T) < 16) attend_launch<T, 64, true>(p, c, layer, wk, a, st);
-    else if (p.dp == 64) attend_launch<T, 64, false>(p, c, layer, wk, a, st);
-    else if (p.dp == 128) attend_launch<T, 128, false>(p, c, layer, wk, a, st);
-    else attend_launch<T, 256, false>(p, c, layer, wk, a, st);
+    if (c.D * sizeof(T) < 16) attend_waves<T, 64, true>(p, c, layer, wk, a, st);
+    else if (p.dp == 64) attend_waves<T, 64, false>(p, c, layer, wk, a, st);
+    else if (p.dp == 128) attend_waves<T, 128, false>(p, c, layer, wk, a, st);
+    else attend_launch<T, 256, kWaves, false>(p, c, layer, wk, a, st);
 }
 
 }  // namespace
