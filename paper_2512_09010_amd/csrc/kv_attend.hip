@@ -46,7 +46,7 @@ constexpr int kMaxSplits = 256;
 constexpr float kLogE = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
-constexpr int kWaves = 4, kMoreWaves = 8;
+constexpr int kWaves = 4;
 
 __device__ __forceinline__ float xor16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32, kWave); }
@@ -85,13 +85,13 @@ struct KvWork {
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
 
-// DP: channels with room (64, 128, 256); NW: wavefronts; SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
-template <typename T, int DP, int NW, bool SMALL, bool SIZED>
-__global__ void __launch_bounds__(NW * 64, DP == 256 ? 1 : DP == 64 ? 4 : sizeof(T) == 4 || NW == kMoreWaves ? 2 : 3)
+// DP: channels with room (64, 128, 256); SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
+template <typename T, int DP, bool SMALL, bool SIZED>
+__global__ void __launch_bounds__(kWaves * 64, DP == 256 ? 1 : DP == 64 ? 4 : sizeof(T) == 4 ? 2 : 3)
 kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, KvAttend a)
 {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int ES = (int)sizeof(T), NT = NW * 64;
+    constexpr int ES = (int)sizeof(T), NW = kWaves, NT = NW * 64;
     constexpr int TILES = BF ? 2 : 1, TOK = 16 * TILES, STEP = NW * TOK;      // tokens of a wavefront's step, of the workgroup's
     constexpr int KE = 16 / ES;                               // elements in 16 bytes
     constexpr int NK = DP / (4 * KE);                         // pieces of a key per lane
@@ -506,18 +506,18 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes,
     int64_t best = std::min<int64_t>(fewest, all);
     double least = 1e300;
     for (int64_t n = best; n <= std::min<int64_t>(most, all); n += n < 4 ? 1 : n / 4) {
-        const int64_t runs = (all + n - 1) / n, each = (rows * tiles * runs + 255) / 256;
-        const double memory = (double)rows * all * step_bytes / 5.9e6, steps = n * step_us * (resident > 1 ? 1.0 + 0.4 * (double)each : 1.4 * (double)each);
+        const int64_t runs = (all + n - 1) / n, each = (rows * tiles * runs + 255) / 256, even = (all + runs - 1) / runs;
+        const double memory = (double)rows * all * step_bytes / 5.9e6, steps = (double)even * step_us * (resident > 1 ? 1.0 + 0.4 * (double)each : 1.4 * (double)each);
         const double us = runs == 1 ? std::max(memory, steps)
-                                    : std::max({memory * (1.0 + 0.25 / std::sqrt((double)n)), steps, 0.33 * (double)runs}) + 4.0 + 0.6 * (double)((runs - 1) / (16 * groups));
-        if (us < least) { least = us; best = n; }
+                                    : std::max({memory * (1.0 + 0.25 / std::sqrt((double)n)), steps, 0.33 * (double)runs}) + 2.5 + 0.6 * (double)((runs - 1) / (8 * groups));
+        if (us < least) { least = us; best = even; }
     }
     return (int)best;
 }
 
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, waves, tiles, cols, chunk, splits, parts_row, lds_words;
+    int dp, tiles, cols, chunk, splits, parts_row, lds_words;
     int64_t rows;
     unsigned blocks;
     size_t words, bytes, lds;
@@ -531,48 +531,38 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
     const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
-    // up to four steps of twice the wavefronts need no join, which is worth more than four steps take, where every workgroup has a unit
-    // of its own (1 x 208 tokens, 32 heads of 128, fp32: 9.4 us joined, JOINED)
-    p.waves = p.dp < 256 && all > 1 && all <= 8 && p.rows * p.tiles <= 256 ? kMoreWaves : kWaves;
-    p.chunk = (p.waves == kMoreWaves ? (all + 1) / 2 * 2 : attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2)) * step;
+    p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2) * step;
     p.splits = (max_tokens + p.chunk - 1) / p.chunk;
     p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
     p.words = align_up((size_t)p.rows * p.tiles * sizeof(tile_tag_t));
     p.bytes = p.words + (p.splits > 1 ? align_up((size_t)p.rows * p.tiles * p.splits * p.cols * p.parts_row * sizeof(float)) : 0);
     // keys and queries; parts of the wavefronts; partial sums over runs.  Then maxima, sums, a word
-    const size_t front = (size_t)(p.waves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)p.waves * p.cols * (p.dp + 4) * sizeof(float);
-    const size_t join = p.splits > 1 ? (size_t)p.waves * 64 * 8 * sizeof(float) : 0;
+    const size_t front = (size_t)(kWaves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)kWaves * p.cols * (p.dp + 4) * sizeof(float);
+    const size_t join = p.splits > 1 ? (size_t)kWaves * 64 * 8 * sizeof(float) : 0;
     size_t most = front > parts ? front : parts;
     most = most > join ? most : join;
     p.lds_words = (int)align_up(most, 16);
-    p.lds = p.lds_words + (2 * (size_t)p.waves * 16 + 4) * sizeof(float);
+    p.lds = p.lds_words + (2 * (size_t)kWaves * 16 + 4) * sizeof(float);
     return p;
 }
 
-template <typename T, int DP, int NW, bool SMALL>
+template <typename T, int DP, bool SMALL>
 void attend_launch(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
     const T *k = (const T*)c.k + layer * c.layer_stride, *v = (const T*)c.v + layer * c.layer_stride;
-    const dim3 grid(p.blocks), block(NW * 64);
-    if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, NW, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
-    else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, NW, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
-}
-
-template <typename T, int DP, bool SMALL>
-void attend_waves(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
-{
-    if (p.waves == kMoreWaves) attend_launch<T, DP, kMoreWaves, SMALL>(p, c, layer, wk, a, st);
-    else attend_launch<T, DP, kWaves, SMALL>(p, c, layer, wk, a, st);
+    const dim3 grid(p.blocks), block(kWaves * 64);
+    if (c.sizes) LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, true>), grid, block, p.lds, st, k, v, wk, a);
+    else LUVC_LAUNCH("kv_attend", (kv_attend<T, DP, SMALL, false>), grid, block, p.lds, st, k, v, wk, a);
 }
 
 template <typename T>
 void attend_shape(const AttendPlan& p, const luvc_kv_cache& c, int layer, const KvWork& wk, const KvAttend& a, hipStream_t st)
 {
-    if (c.D * sizeof(T) < 16) attend_waves<T, 64, true>(p, c, layer, wk, a, st);
-    else if (p.dp == 64) attend_waves<T, 64, false>(p, c, layer, wk, a, st);
-    else if (p.dp == 128) attend_waves<T, 128, false>(p, c, layer, wk, a, st);
-    else attend_launch<T, 256, kWaves, false>(p, c, layer, wk, a, st);
+    if (c.D * sizeof(T) < 16) attend_launch<T, 64, true>(p, c, layer, wk, a, st);
+    else if (p.dp == 64) attend_launch<T, 64, false>(p, c, layer, wk, a, st);
+    else if (p.dp == 128) attend_launch<T, 128, false>(p, c, layer, wk, a, st);
+    else attend_launch<T, 256, false>(p, c, layer, wk, a, st);
 }
 
 }  // namespace
