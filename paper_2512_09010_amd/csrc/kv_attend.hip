@@ -42,7 +42,7 @@ template <> struct kv_piece_t<bf16_t, 4> { typedef uint32_t type __attribute__((
 template <> struct kv_piece_t<bf16_t, 2> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
 typedef int32_t kv_sizes4 __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int kMaxSplits = 256;
+constexpr int kMaxSplits = 256, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
 constexpr float kLogE = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
@@ -76,10 +76,11 @@ __device__ __forceinline__ void load_words(uint32_t* w, const char* rows, uint32
 struct KvWork {
     const int32_t* sizes;
     int n_pages, n_heads, log2_page, D, group, chunk, tiles, cols, parts_row;      // tiles of at most `cols` query heads; parts_row: floats
+    int words_each;
     int lds_words;                   // where the maxima and sums of the wavefronts lie in LDS
     unsigned rows, splits;           // sequences x cache heads; the most runs of one
     float* parts;                    // [rows, tiles, splits, cols, parts_row]
-    tile_tag_t* words;               // [rows, tiles]
+    tile_tag_t* words;               // [rows, tiles, words_each]
     tile_tag_t tag;
     float scale;                     // of the logits, to powers of two; positive
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
@@ -147,9 +148,14 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     len = len < 0 ? 0 : len > room ? room : len;
     const int splits = len > wk.chunk ? (len + wk.chunk - 1) / wk.chunk : 1;
     if (split >= splits) return;
-    tile_tag_t* word = wk.words + ((int64_t)row * wk.tiles + qt);
-    tile_tag_t seen = 0;
-    if (splits > 1 && tid == 0) seen = tag_load(word);
+    // Arrival words: the sequence's, then those of its groups of runs.  A word is the process's tag and a count; one without the tag is
+    // taken over by whoever may come to it first (thread 0: the word of this run; thread 1 of a group's first run: the sequence's, to which
+    // the group comes when all of it has arrived), and whoever completes a count leaves the tag and zero behind.
+    const bool grouped = splits > kDirect;
+    tile_tag_t* const words = wk.words + ((int64_t)row * wk.tiles + qt) * wk.words_each;
+    tile_tag_t* word = words + (grouped ? 1 + split / kFan : 0);
+    tile_tag_t* const claimed = splits > 1 && tid == 0 ? word : grouped && tid == 1 && split % kFan == 0 ? words : nullptr;
+    const tile_tag_t seen = claimed ? tag_load(claimed) : 0;
     const int end = split == splits - 1 ? len : (split + 1) * wk.chunk;
 
     // Keys as the product wants them, 16 bytes of one token per lane and the tokens in neighbouring lanes, would be 64 places to look
@@ -372,9 +378,9 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                     *(kv_f32x4*)&so[(wave * wk.cols + c) * LD + (16 * n + 4 * g + i) * VL + e] = w;
                 }
     }
-    if (splits > 1 && tid == 0 && (seen >> 16) != wk.tag) {
+    if (claimed && (seen >> 16) != wk.tag) {
         tile_tag_t expect = seen;
-        (void)__hip_atomic_compare_exchange_strong(word, &expect, wk.tag << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        (void)__hip_atomic_compare_exchange_strong(claimed, &expect, wk.tag << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     // Four channels of a head to a thread, in the order of heads of DP channels; further rows of threads, where heads are few, share runs
@@ -423,6 +429,11 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         }
         __device__ __forceinline__ kv_f32x4 mean() const { return v * (sum > 0.f ? 1.f / sum : 0.f); }
     };
+    auto keep = [&](int run, int col, int d, const Sum& t) {
+        const uint32_t at = (uint32_t)((run * part + col * wk.parts_row) * 4);
+        tile_vec<4>::store(__builtin_bit_cast(tile_vec<4>::type, t.v), all, at + d * 4);
+        if (d == 0) tile_vec<2>::store(tile_vec<2>::type{__float_as_uint(t.top), __float_as_uint(t.sum)}, all, at + (wk.parts_row - 4) * 4);
+    };
     if (grp == 0)
         for (int i = item0; i < nh * QUADS; i += NT) {
             const int col = i / QUADS, d = i % QUADS * 4;
@@ -430,86 +441,98 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
             Sum t{sm[0][col], sl[0][col], part_of(&so[col * LD], d)};
 #pragma unroll
             for (int w = 1; w < NW; ++w) t.add(sm[w][col], sl[w][col], part_of(&so[(w * wk.cols + col) * LD], d));
-            if (splits == 1) {
-                store(col, d, t.mean());
-            } else {
-                const uint32_t at = (uint32_t)((split * part + col * wk.parts_row) * 4);
-                tile_vec<4>::store(__builtin_bit_cast(tile_vec<4>::type, t.v), all, at + d * 4);
-                if (d == 0) tile_vec<2>::store(tile_vec<2>::type{__float_as_uint(t.top), __float_as_uint(t.sum)}, all, at + (wk.parts_row - 4) * 4);
-            }
+            if (splits == 1) store(col, d, t.mean());
+            else keep(split, col, d, t);
         }
     if (splits == 1) return;
 
-    // ---- the runs of the sequence, by the workgroup that ends last
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        const tile_tag_t old = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last_flag = (int)(old & 0xffffu) == splits - 1;
-        if (last_flag) tag_store(word, wk.tag << 16);
-    }
-    __syncthreads();
-    if (!last_flag) return;
-    constexpr int AHEAD = 8;                                  // runs of a thread in flight
-    for (int i0 = 0; i0 < nh * QUADS; i0 += NT) {
-        const int i = i0 + item0, col = i / QUADS, d = i % QUADS * 4;
-        const bool in = col < nh && d < D;
-        const uint32_t at = in ? (uint32_t)(col * wk.parts_row * 4) : 0u;
-        Sum t{kLowest, 0.f, {}};
-#pragma unroll 1
-        for (int k0 = grp; k0 < splits; k0 += AHEAD * groups) {
-            tile_vec<4>::type x[AHEAD];
-            tile_vec<2>::type ml[AHEAD];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int run = k0 + k * groups;
-                const uint32_t from = (uint32_t)((run < splits ? run : splits - 1) * part * 4) + at;
-                x[k] = tile_vec<4>::load(all, from + (in ? d * 4 : 0));
-                ml[k] = tile_vec<2>::load(all, from + (wk.parts_row - 4) * 4);
-            }
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const bool there = k0 + k * groups < splits;
-                t.add(there ? __uint_as_float(ml[k][0]) : kLowest, there ? __uint_as_float(ml[k][1]) : 0.f, there ? __builtin_bit_cast(kv_f32x4, x[k]) : kv_f32x4{});
-            }
+    // ---- the runs of the sequence, or first those of its groups, by the workgroup that ends last
+    int first = grouped ? split / kFan * kFan : 0, runs = !grouped ? splits : splits - first < kFan ? splits - first : kFan, apart = 1;
+    for (bool done = !grouped;; done = true) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+            const tile_tag_t old = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last_flag = (int)(old & 0xffffu) == runs - 1;
+            if (last_flag) tag_store(word, wk.tag << 16);
         }
-        if (groups > 1) {                                     // nh * QUADS < NT: one round
-            float* red = so + tid * 8;
-            *(kv_f32x4*)red = t.v;
-            red[4] = t.top;
-            red[5] = t.sum;
-            __syncthreads();
+        __syncthreads();
+        if (!last_flag) return;
+        constexpr int AHEAD = 8;                              // runs of a thread in flight
+        for (int i0 = 0; i0 < nh * QUADS; i0 += NT) {
+            const int i = i0 + item0, col = i / QUADS, d = i % QUADS * 4;
+            const bool in = col < nh && d < D;
+            const uint32_t at = (uint32_t)((first * part + (in ? col * wk.parts_row : 0)) * 4);
+            Sum t{kLowest, 0.f, {}};
 #pragma unroll 1
-            for (int k = 1; grp == 0 && k < groups; ++k) {
-                red += 8 << log2_items;
-                t.add(red[4], red[5], *(const kv_f32x4*)red);
+            for (int k0 = grp; k0 < runs; k0 += AHEAD * groups) {
+                tile_vec<4>::type x[AHEAD];
+                tile_vec<2>::type ml[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int run = k0 + k * groups;
+                    const uint32_t from = (uint32_t)((run < runs ? run : runs - 1) * apart * part * 4) + at;
+                    x[k] = tile_vec<4>::load(all, from + (in ? d * 4 : 0));
+                    ml[k] = tile_vec<2>::load(all, from + (wk.parts_row - 4) * 4);
+                }
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const bool there = k0 + k * groups < runs;
+                    t.add(there ? __uint_as_float(ml[k][0]) : kLowest, there ? __uint_as_float(ml[k][1]) : 0.f, there ? __builtin_bit_cast(kv_f32x4, x[k]) : kv_f32x4{});
+                }
             }
+            if (groups > 1) {                                 // nh * QUADS < NT: one round
+                float* red = so + tid * 8;
+                *(kv_f32x4*)red = t.v;
+                red[4] = t.top;
+                red[5] = t.sum;
+                __syncthreads();
+#pragma unroll 1
+                for (int k = 1; grp == 0 && k < groups; ++k) {
+                    red += 8 << log2_items;
+                    t.add(red[4], red[5], *(const kv_f32x4*)red);
+                }
+            }
+            if (!in || grp) continue;
+            if (done) store(col, d, t.mean());
+            else keep(first, col, d, t);
         }
-        if (in && grp == 0) store(col, d, t.mean());
+        if (done) return;
+        // the groups' sums are in the places of their first runs
+        first = 0;
+        runs = (splits + kFan - 1) / kFan;
+        apart = kFan;
+        word = words;
     }
 }
 
-// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  All measured:
-// memory keeps up with 5.9 TB/s of steps, less a share for the parts of runs that are joined and for workgroups that come and go; a
-// workgroup that is alone on its unit takes a step of 64 KB in 1.4 us; runs arrive at a word one every third of a microsecond; the join takes
-// 4 us and 0.6 more for every further trip to memory (1 x 32768 tokens, 8 heads of 128, bf16, 256 steps: 45.8 us with 32 steps to a
-// workgroup, 30.0 with 16, 28.3 with 12, 28.9 with 8, 31.3 with 4, 48 with 2, 91 with 1; 8 x 1100, 4 heads, 9 steps: 10.4 with
-// 1, 9.7 with 2, 10.5 with 4, 11.2 with 9).  At most 8 (1024 tokens in bf16) where that leaves two workgroups to a unit: `all` is
-// a bound, and one sequence of that length among short ones would be waited for (64 sequences of 1 to 8200 tokens, 8 heads: 86 us with 16
-// steps, 75 with 8; 64 of 4096 lose 194 for 180).
-int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes, int resident)
+// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  All measured, on tokens
+// that come from HBM:
+//   - memory delivers 5.9 TB/s, less a share for the parts of runs that are joined and for workgroups that come and go;
+//   - a compute unit takes a step of 64 KB in 1.6 us, in 1.7 where it has two workgroups or more: one workgroup too many for the units
+//     doubles the time of some (100000 tokens, 4 heads of 128, bf16, 782 steps: 37.2 us with 196 workgroups of 16 steps, 49.1 with
+//     264 of 12, 42.3 with 392 of 8);
+//   - joining runs takes 2.5 us and 1.2 for every further trip to memory, in groups twice that.
+// (1 x 32768 tokens, 8 heads, 256 steps: 43.6 us with 32 steps to a workgroup, 27.6 with 16, 25.8 with 12, 26.1 with 8, 26.9 with 4, 33.0 with
+// 2, 42.9 with 1; 8 x 1100, 4 heads, 9 steps: 10.2 with 1, 8.4 with 2, 10.4 with 4, 13.3 with 9.)
+// At most 8 (1024 tokens in bf16) where that leaves two workgroups to a unit: `all` is a bound, and one sequence of that length among
+// short ones would be waited for (64 sequences of 1 to 8200 tokens, 8 heads: 78 us with 16 steps, 69 with 8; 64 of 4096 lose 169 for 158).
+int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
 {
     const int64_t fewest = std::max<int64_t>((all + kMaxSplits - 1) / kMaxSplits, (rows * tiles * all >> 22) + 1);
     const int64_t most = rows * tiles * ((all + 7) / 8) >= 512 ? 8 : all;
-    const int groups = quads < kWaves * 64 ? kWaves * 64 / quads : 1;
-    const double step_us = std::max(0.5, step_bytes / 65536.0);
+    const int64_t at_once = 8 * (quads < kWaves * 64 ? kWaves * 64 / quads : 1);
+    const double step_us = std::max(0.5, step_bytes / 65536.0), memory = (double)rows * all * step_bytes / 5.9e6;
     int64_t best = std::min<int64_t>(fewest, all);
     double least = 1e300;
     for (int64_t n = best; n <= std::min<int64_t>(most, all); n += n < 4 ? 1 : n / 4) {
         const int64_t runs = (all + n - 1) / n, each = (rows * tiles * runs + 255) / 256, even = (all + runs - 1) / runs;
-        const double memory = (double)rows * all * step_bytes / 5.9e6, steps = (double)even * step_us * (resident > 1 ? 1.0 + 0.4 * (double)each : 1.4 * (double)each);
-        const double us = runs == 1 ? std::max(memory, steps)
-                                    : std::max({memory * (1.0 + 0.25 / std::sqrt((double)n)), steps, 0.33 * (double)runs}) + 2.5 + 0.6 * (double)((runs - 1) / (8 * groups));
+        const double steps = (double)(even * each) * step_us * (each > 1 ? 1.7 : 1.6);
+        double us = memory;
+        if (runs > 1) us *= 1.0 + 0.25 / std::sqrt((double)even);
+        us = std::max(us, steps);
+        if (runs > kDirect) us += 5.0 + 1.2 * (double)((kFan - 1) / at_once + (runs - 1) / kFan / at_once);
+        else if (runs > 1) us += 2.5 + 1.2 * (double)((runs - 1) / at_once);
         if (us < least) { least = us; best = even; }
     }
     return (int)best;
@@ -517,7 +540,7 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes,
 
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, tiles, cols, chunk, splits, parts_row, lds_words;
+    int dp, tiles, cols, chunk, splits, parts_row, lds_words, words_each;
     int64_t rows;
     unsigned blocks;
     size_t words, bytes, lds;
@@ -531,11 +554,12 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
     const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
-    p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es, p.dp == 256 ? 1 : 2) * step;
+    p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
     p.splits = (max_tokens + p.chunk - 1) / p.chunk;
     p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
-    p.words = align_up((size_t)p.rows * p.tiles * sizeof(tile_tag_t));
+    p.words_each = p.splits > kDirect ? 1 + (p.splits + kFan - 1) / kFan : 1;
+    p.words = align_up((size_t)p.rows * p.tiles * p.words_each * sizeof(tile_tag_t));
     p.bytes = p.words + (p.splits > 1 ? align_up((size_t)p.rows * p.tiles * p.splits * p.cols * p.parts_row * sizeof(float)) : 0);
     // keys and queries; parts of the wavefronts; partial sums over runs.  Then maxima, sums, a word
     const size_t front = (size_t)(kWaves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)kWaves * p.cols * (p.dp + 4) * sizeof(float);
@@ -576,7 +600,7 @@ luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, 
 {
     const AttendPlan p = attend_plan(a.n_seqs, a.n_q_heads, c.n_heads, c.D, c.dtype, a.max_tokens);
     static const tile_tag_t tag = spu_next_tag();
-    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.lds_words, (unsigned)p.rows, (unsigned)p.splits,
+    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, (unsigned)p.rows, (unsigned)p.splits,
                     (float*)((char*)ws + p.words), (tile_tag_t*)ws, tag,
                     a.scale == 0.f ? 1.f : std::fabs(a.scale) * kLogE, a.scale < 0.f ? -1 : a.scale > 0.f};
     if (c.dtype == LUVC_F32) attend_shape<float>(p, c, layer, wk, a, st);
