@@ -92,6 +92,11 @@ SHAPES = [
     ([1500], 8, 1, 32, "bf16", 16, "mask"),
     ([5000, 3, 2500], 8, 2, 128, "bf16", 16, "enhance"),
     ([5000, 3, 2500], 8, 2, 64, "f32", 64, "mask"),
+    # runs that are joined in groups, next to sequences of a few runs, of one, of none
+    ([40000, 3000, 100, 0], 4, 1, 64, "bf16", 16, "none"),
+    ([30000, 2000, 700], 2, 1, 100, "bf16", 64, "enhance"),
+    ([20000, 11, 9000], 1, 1, 128, "f32", 32, "mask"),
+    ([25000], 19, 1, 24, "bf16", 256, "mask"),
 ]
 
 
@@ -196,13 +201,14 @@ def test_attend_beyond_32_bits():
     torch.cuda.empty_cache()
 
 
-def test_attend_with_stale_workspaces_streams_and_repeats():
+@pytest.mark.parametrize("long", [False, True])
+def test_attend_with_stale_workspaces_streams_and_repeats(long):
     """Same bits whatever the workspace held, on other streams at once, call after call."""
-    pool = Pool(7, [3000, 1, 700, 0, 2900, 64], 2, 128, "bf16", 16)
-    q = pool.tensor(6, 8, 128)
+    pool = Pool(7, [3000, 1, 700, 0, 2900, 64] if not long else [30000, 1, 700, 0, 2900, 64], 1 if long else 2, 128, "bf16", 16)
+    q, most = pool.tensor(6, 8, 128), 16 * pool.width
     want = lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, enhance=True)
     check_attend(pool, q, want, enhance=True)
-    need = lv.luvc_kv_attend_workspace_bytes(pool.cache, 6, 8, 3008)
+    need = lv.luvc_kv_attend_workspace_bytes(pool.cache, 6, 8, most)
     gen = torch.Generator(device="cuda").manual_seed(3)
     streams = [torch.cuda.Stream() for _ in range(3)]
     spaces = [torch.randint(0, 256, (need,), generator=gen, dtype=torch.uint8, device="cuda") for _ in streams]
@@ -210,9 +216,9 @@ def test_attend_with_stale_workspaces_streams_and_repeats():
     torch.cuda.synchronize()
     for i in range(8):
         for st, ws, o in zip(streams, spaces, outs):
-            lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, max_tokens=3008, enhance=True, workspace=ws, out=o[i], stream=st)
+            lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, max_tokens=most, enhance=True, workspace=ws, out=o[i], stream=st)
     torch.cuda.synchronize()
-    again = lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, max_tokens=3008, enhance=True)
+    again = lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, max_tokens=most, enhance=True)
     for o in outs:
         for t in o:
             assert torch.equal(t, again)
