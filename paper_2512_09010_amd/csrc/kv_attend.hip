@@ -78,13 +78,86 @@ struct KvWork {
     int n_pages, n_heads, log2_page, D, group, chunk, tiles, cols, parts_row;      // tiles of at most `cols` query heads; parts_row: floats
     int words_each;
     int lds_words;                   // where the maxima and sums of the wavefronts lie in LDS
-    unsigned rows, splits;           // sequences x cache heads; the most runs of one
-    float* parts;                    // [rows, tiles, splits, cols, parts_row]
+    bool planned;                    // runs by the lengths
+    int fewest;                      // steps of a run, at least
+    unsigned rows, splits, units;    // sequences x cache heads; the most runs of one; runs of all in the grid
+    float* parts;                    // [runs x heads x tiles, cols, parts_row], the runs of one head of a sequence one after the other
     tile_tag_t* words;               // [rows, tiles, words_each]
     tile_tag_t tag;
     float scale;                     // of the logits, to powers of two; positive
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
+
+// Runs by the lengths, which every wavefront of the grid works out for itself: the steps of all sequences decide how many steps a run has,
+// one workgroup to a compute unit where the runs of up to 16 steps can be cut like that (one too many is a unit with twice the work: a few
+// longer runs are tried), two where not; a sequence's runs are of equal length.  Those of sequences with several come before the
+// sequences of one run: the long ones first.  64 sequences of 1 to 8200 tokens, 8 heads of 128, bf16: 68.5 us with runs by the bound, of
+// which 3500 in 4600 were empty and kept others waiting, 57 like this; it is a trip to memory more, 0.7 us.
+// kPlanUnits / n_parts + n runs at most, n <= 256 sequences.  Sequence 4 lane + k (or fewer to a lane) belongs to a lane.
+constexpr int kPlanUnits = 512, kPlanSeqs = 256;
+struct RunOf { int seq, run, runs, chunk, len, before; };     // before: runs of the sequences in front
+inline __host__ __device__ int plan_runs(int n_parts) { return (kPlanUnits + n_parts - 1) / n_parts; }
+__device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, int x, int room, int step, int n_parts, int fewest, int lane)
+{
+    const int per = (n + 63) / 64;
+    int len[kPlanSeqs / 64], runs[kPlanSeqs / 64];
+    float steps = 0.f;
+#pragma unroll
+    for (int k = 0; k < kPlanSeqs / 64; ++k) {
+        if (k >= per) break;
+        const int i = lane * per + k;
+        const int l = i < n ? lengths[i] : -1;
+        len[k] = i >= n ? -1 : l < 0 ? 0 : l > room ? room : l;
+        steps += (float)((len[k] + step - 1) / step);
+    }
+    // no rounding of the sum may make it smaller than it is: the runs have to fit the grid
+    steps = wave_sum(steps) * 1.0001f;
+    const float one = steps * (float)n_parts / (kPlanUnits / 2), two = steps / (float)plan_runs(n_parts);
+    int each = (int)ceilf(one <= 16.f ? one : two), left = one <= 16.f ? 3 : 0;
+    const int more = each < 10 ? 1 : each / 10;
+    uint32_t mine, upto, total;
+    for (;; each += more) {
+        if (each < fewest) each = fewest;
+        mine = 0;                                             // runs of sequences with several, sequences with one
+#pragma unroll
+        for (int k = 0; k < kPlanSeqs / 64; ++k) {
+            if (k >= per) break;
+            const int a = (len[k] + step - 1) / step;
+            runs[k] = len[k] < 0 ? 0 : a <= each ? 1 : (a + each - 1) / each;
+            mine += runs[k] > 1 ? (uint32_t)runs[k] << 16 : (uint32_t)runs[k];
+        }
+        upto = wave_scan_incl(mine);
+        total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        if (left == 0 || ((total >> 16) + (total & 0xffffu)) * n_parts <= kPlanUnits / 2) break;
+        if (--left == 0) each = (int)ceilf(two) - more;
+    }
+    const int several = (int)(total >> 16);
+    RunOf r{-1, 0, 0, 0, 0, 0};
+    if (x >= several + (int)(total & 0xffffu)) return r;
+    const bool long_one = x < several;
+    const int y = long_one ? x : x - several;
+    int at = long_one ? (int)((upto - mine) >> 16) : (int)((upto - mine) & 0xffffu);
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < kPlanSeqs / 64; ++k) {
+        if (k >= per) break;
+        const int here = (runs[k] > 1) == long_one ? runs[k] : 0;
+        if (y >= at && y < at + here) {
+            found = true;
+            r = RunOf{lane * per + k, y - at, here, 0, len[k], at + (long_one ? 0 : several)};
+        }
+        at += here;
+    }
+    const int src = __ffsll((long long)__ballot(found)) - 1;
+    r.seq = __builtin_amdgcn_readlane(r.seq, src);
+    r.run = __builtin_amdgcn_readlane(r.run, src);
+    r.runs = __builtin_amdgcn_readlane(r.runs, src);
+    r.len = __builtin_amdgcn_readlane(r.len, src);
+    r.before = __builtin_amdgcn_readlane(r.before, src);
+    const int a = (r.len + step - 1) / step;
+    r.chunk = (a + r.runs - 1) / r.runs * step;
+    return r;
+}
 
 // DP: channels with room (64, 128, 256); SMALL: rows shorter than 16 bytes; SIZED: the cache has sizes
 template <typename T, int DP, bool SMALL, bool SIZED>
@@ -107,24 +180,42 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // runs before rows, so that long sequences' later runs come last; tiles of one run read the same tokens: eight workgroups apart they
-    // meet in the L2 of one XCD
+    // tiles of one run read the same tokens: eight workgroups apart they meet in the L2 of one XCD
     const unsigned band = blockIdx.x / (8 * wk.tiles), in_band = blockIdx.x % (8 * wk.tiles), unit = band * 8 + in_band % 8;
-    const int qt = in_band / 8, split = unit / wk.rows, row = unit % wk.rows;
-    if (unit >= wk.rows * wk.splits) return;
-    const int h = row % wk.n_heads, s = row / wk.n_heads, D = wk.D;
-
-    // what does not depend on one another is asked for together: the length, the first pages, the queries
+    const int qt = in_band / 8, D = wk.D;
+    if (unit >= wk.units) return;
     const int64_t held = (int64_t)a.max_pages << wk.log2_page;
     const int room = held < a.max_tokens ? (int)held : a.max_tokens;
+    // Which run of which sequence and cache head: by the bound on the lengths alone, or, where several sequences differ, by their lengths
+    int s, h, split, splits = 0, chunk = wk.chunk, len;
+    int64_t slot;                                             // of the sequence's first run among the parts
+    if (wk.planned) {
+        const RunOf r = run_by_lengths(a.lengths, a.n_seqs, unit / wk.n_heads, room, STEP, wk.n_heads * wk.tiles, wk.fewest, lane);
+        if (r.seq < 0) return;
+        s = r.seq;
+        h = unit % wk.n_heads;
+        split = r.run;
+        splits = r.runs;
+        chunk = r.chunk;
+        len = r.len;
+        slot = (int64_t)r.before * (wk.n_heads * wk.tiles) + (h * wk.tiles + qt) * splits;
+    } else {
+        const int row = unit % wk.rows;
+        split = unit / wk.rows;
+        h = row % wk.n_heads;
+        s = row / wk.n_heads;
+        len = as_scalars(a.lengths)[s];
+        slot = ((int64_t)row * wk.tiles + qt) * wk.splits;
+    }
+
+    // what does not depend on one another is asked for together: the length, the first pages, the queries
     const scalar_words table = as_scalars(a.table) + (int64_t)s * a.max_pages;
-    int t0 = split * wk.chunk + wave * TOK;
+    int t0 = split * chunk + wave * TOK;
     struct Pages { int first, second; };                      // of a step's tiles
     auto page_at = [&](int t) { return table[(t < room ? t : room - 1) >> wk.log2_page]; };      // behind the end any will do: nothing there is live
     auto pages_at = [&](int t) { return Pages{page_at(t), TILES > 1 ? page_at(t + 16) : 0}; };
     const Pages pages0 = pages_at(t0);
     Pages pages1 = pages_at(t0 + STEP), pages2 = pages_at(t0 + 2 * STEP);
-    int len = as_scalars(a.lengths)[s];
     // Query heads head0 .. head0 + nh - 1 of the call are columns of the products, zeros behind them.  A piece that would reach beyond a
     // row, of queries, keys or values, is the row's last one instead: what it repeats is zero among the queries, and of the values
     // it makes the same channels of the output once more.
@@ -145,18 +236,20 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         }
         *(kv_u32x4*)(queries + (col * (PIECES + 1) + i % PIECES) * 16) = kv_u32x4{w[0], w[1], w[2], w[3]};
     }
-    len = len < 0 ? 0 : len > room ? room : len;
-    const int splits = len > wk.chunk ? (len + wk.chunk - 1) / wk.chunk : 1;
-    if (split >= splits) return;
+    if (!wk.planned) {
+        len = len < 0 ? 0 : len > room ? room : len;
+        splits = len > chunk ? (len + chunk - 1) / chunk : 1;
+        if (split >= splits) return;
+    }
     // Arrival words: the sequence's, then those of its groups of runs.  A word is the process's tag and a count; one without the tag is
     // taken over by whoever may come to it first (thread 0: the word of this run; thread 1 of a group's first run: the sequence's, to which
     // the group comes when all of it has arrived), and whoever completes a count leaves the tag and zero behind.
     const bool grouped = splits > kDirect;
-    tile_tag_t* const words = wk.words + ((int64_t)row * wk.tiles + qt) * wk.words_each;
+    tile_tag_t* const words = wk.words + (((int64_t)s * wk.n_heads + h) * wk.tiles + qt) * wk.words_each;
     tile_tag_t* word = words + (grouped ? 1 + split / kFan : 0);
     tile_tag_t* const claimed = splits > 1 && tid == 0 ? word : grouped && tid == 1 && split % kFan == 0 ? words : nullptr;
     const tile_tag_t seen = claimed ? tag_load(claimed) : 0;
-    const int end = split == splits - 1 ? len : (split + 1) * wk.chunk;
+    const int end = split == splits - 1 ? len : (split + 1) * chunk;
 
     // Keys as the product wants them, 16 bytes of one token per lane and the tokens in neighbouring lanes, would be 64 places to look
     // up per load; as neighbouring lanes read them here, rows, they are 16 or fewer, and LDS turns them round.  Piece p of row r lies at
@@ -388,7 +481,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     const int log2_items = 31 - __builtin_clz(QUADS) + (nh > 1 ? 32 - __builtin_clz(nh - 1) : 0), part = wk.cols * wk.parts_row;
     const int groups = (1 << log2_items) < NT ? NT >> log2_items : 1, grp = groups > 1 ? tid >> log2_items : 0;
     const int item0 = groups > 1 ? tid & ((1 << log2_items) - 1) : tid;
-    float* parts = wk.parts + ((int64_t)row * wk.tiles + qt) * wk.splits * part;
+    float* parts = wk.parts + slot * part;
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(parts, 0, splits * part * 4, 0x00020000);
     auto store = [&](int col, int d, kv_f32x4 v) {
         T* out = (T*)a.out + s * a.out_stride + (int64_t)(head0 + col) * D + d;
@@ -540,8 +633,9 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
 
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, tiles, cols, chunk, splits, parts_row, lds_words, words_each;
-    int64_t rows;
+    int dp, tiles, cols, chunk, splits, parts_row, lds_words, words_each, fewest;
+    bool planned;
+    int64_t rows, units, slots;
     unsigned blocks;
     size_t words, bytes, lds;
 };
@@ -554,13 +648,26 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.cols = group < 16 ? group : 16;
     p.rows = (int64_t)n_seqs * n_heads;
     const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
-    p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
-    p.splits = (max_tokens + p.chunk - 1) / p.chunk;
-    p.blocks = (unsigned)((p.rows * p.splits + 7) / 8 * 8 * p.tiles);
+    const int n_parts = n_heads * p.tiles;
+    p.planned = n_seqs > 1 && n_seqs <= kPlanSeqs && p.rows * p.tiles * all > 512;
+    p.fewest = (all + kMaxSplits - 1) / kMaxSplits;
+    if (p.planned) {
+        const int64_t runs = std::min<int64_t>((int64_t)n_seqs * all, plan_runs(n_parts) + n_seqs);
+        p.chunk = 0;
+        p.splits = std::min<int>(kMaxSplits, std::min<int>(all, plan_runs(n_parts) + 1));
+        p.units = runs * n_heads;
+        p.slots = runs * n_parts;
+    } else {
+        p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
+        p.splits = (max_tokens + p.chunk - 1) / p.chunk;
+        p.units = p.rows * p.splits;
+        p.slots = p.splits > 1 ? p.units * p.tiles : 0;
+    }
+    p.blocks = (unsigned)((p.units + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
     p.words_each = p.splits > kDirect ? 1 + (p.splits + kFan - 1) / kFan : 1;
     p.words = align_up((size_t)p.rows * p.tiles * p.words_each * sizeof(tile_tag_t));
-    p.bytes = p.words + (p.splits > 1 ? align_up((size_t)p.rows * p.tiles * p.splits * p.cols * p.parts_row * sizeof(float)) : 0);
+    p.bytes = p.words + align_up((size_t)p.slots * p.cols * p.parts_row * sizeof(float));
     // keys and queries; parts of the wavefronts; partial sums over runs.  Then maxima, sums, a word
     const size_t front = (size_t)(kWaves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)kWaves * p.cols * (p.dp + 4) * sizeof(float);
     const size_t join = p.splits > 1 ? (size_t)kWaves * 64 * 8 * sizeof(float) : 0;
@@ -600,7 +707,8 @@ luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, 
 {
     const AttendPlan p = attend_plan(a.n_seqs, a.n_q_heads, c.n_heads, c.D, c.dtype, a.max_tokens);
     static const tile_tag_t tag = spu_next_tag();
-    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, (unsigned)p.rows, (unsigned)p.splits,
+    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, p.planned, p.fewest,
+                    (unsigned)p.rows, (unsigned)p.splits, (unsigned)p.units,
                     (float*)((char*)ws + p.words), (tile_tag_t*)ws, tag,
                     a.scale == 0.f ? 1.f : std::fabs(a.scale) * kLogE, a.scale < 0.f ? -1 : a.scale > 0.f};
     if (c.dtype == LUVC_F32) attend_shape<float>(p, c, layer, wk, a, st);
