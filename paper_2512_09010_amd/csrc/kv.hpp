@@ -37,7 +37,7 @@ struct KvAttend {
     int64_t q_stride, out_stride;
     const int32_t *table, *lengths;
     int n_seqs, n_q_heads, max_pages, max_tokens;
-    float scale;
+    double scale;
     bool enhance;
 };
 size_t kv_attend_workspace(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype dt, int max_tokens);

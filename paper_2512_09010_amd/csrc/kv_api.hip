@@ -115,8 +115,8 @@ luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q,
     if (q_stride < row || out_stride < row) { set_error("sequence strides must be at least n_q_heads * D = %lld", (long long)row); return LUVC_ERR_INVALID_ARG; }
     if (((uintptr_t)q | (uintptr_t)out) % kv_esize(*cache)) { set_error("q and out must be aligned to their elements"); return LUVC_ERR_INVALID_ARG; }
     if (enhance && !cache->sizes) { set_error("the term log s needs a cache with sizes"); return LUVC_ERR_INVALID_ARG; }
-    const float sc = (float)(scale ? *scale : 1.0 / std::sqrt((double)cache->D));
-    if (!std::isfinite(sc)) { set_error("scale must be finite in fp32"); return LUVC_ERR_INVALID_ARG; }
+    const double sc = scale ? *scale : 1.0 / std::sqrt((double)cache->D);
+    if (!std::isfinite((float)(2.0 * sc))) { set_error("scale must be finite in fp32"); return LUVC_ERR_INVALID_ARG; }
     const size_t need = kv_attend_workspace(n_seqs, n_q_heads, cache->n_heads, cache->D, cache->dtype, max_tokens);
     if (!workspace_ok(workspace, workspace_bytes, need)) return LUVC_ERR_WORKSPACE;
     const KvAttend a{q, out, q_stride, out_stride, table, lengths, n_seqs, n_q_heads, max_pages, max_tokens, sc, enhance != 0};
