@@ -376,13 +376,15 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
  *   q, out      device [n_seqs, n_q_heads, D] dtype with the sequences q_stride / out_stride elements apart (>= n_q_heads * D);
  *               n_q_heads is a multiple of the cache's n_heads
  *   lengths     device [n_seqs] int32; read as min(length, max_tokens, max_pages * page_tokens)
- *   max_tokens  host, >= 1: no sequence is longer; the work is laid out for it, and the workspace
- *   scale       host, or NULL: 1 / sqrt(D)
+ *   max_tokens  host, >= 1: no sequence is longer.  Up to 1024 sequences the work is laid out by their lengths, so that a
+ *               captured call may have a bound far above them; beyond, and for the workspace, by the bound
+ *   scale       host, or NULL: 1 / sqrt(D); twice its value must be finite in fp32
  *   enhance     0: the plain values v_j; else the term log s_j as well (needs a cache with sizes)
  * Logits, softmax and sums are fp32; with bf16 the weights a_j enter the product with the values in two bf16 terms (16 bits)
  * and the output is rounded once.  The parts of a long sequence are joined in a fixed order: same input, same bits.
- * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype); any contents, one per call
- * in flight, also for calls in captured graphs.
+ * Keys and values of the tokens that take part are finite; what the others' places hold does not matter.
+ * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype), which is enough for fewer
+ * sequences and a smaller max_tokens as well; any contents, one per call in flight, also for calls in captured graphs.
  * Limits: n_seqs * n_q_heads < 2^22, max_tokens < 2^30.
  */
 size_t luvc_kv_attend_workspace_bytes(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens);

@@ -2,23 +2,29 @@
 //
 //   z_j = scale <q, k_j>,  m = max z_j,  p_j = exp(z_j - m),  o = (sum p_j v_j + sum p_j log s_j) / sum p_j
 //
-// Every key and value is needed once per query head of its group, 4 G D operations for 2 D elements: HBM bounds it, and the work is to
-// keep loads in flight.  A workgroup of four wavefronts takes a run of tokens of one sequence and cache head, a wavefront TOK
-// of them at a time, with the running maximum and sum of the softmax; all query heads of the group are columns of its products:
-//   S = K Q^T   a tile of 16 tokens x 16 heads (v_mfma_f32_16x16x32_bf16, v_mfma_f32_16x16x4_f32); K rows come from memory as
-//               the operand wants them, 16 bytes of one token per lane
+// Every key and value is needed once, for 4 G D operations on 2 D elements (G query heads to a cache head): HBM bounds it, and the work is to
+// keep loads in flight (64 sequences of 4096 tokens, 32 query heads on 8 of 128, bf16: 1.07 GB in 162 us, 6.6 TB/s, where a large copy
+// reaches 5.1; one sequence of 100000, 4 heads: 205 MB in 38.4 us).  A workgroup of four wavefronts takes a run of tokens of one
+// sequence and cache head, a wavefront TOK of them at a time, with the running maximum and sum of the softmax; all query heads of
+// the group, up to 16, are columns of its products:
+//   S = K Q^T   a tile of 16 tokens x 16 heads (v_mfma_f32_16x16x32_bf16, v_mfma_f32_16x16x4_f32); the rows of K are read as rows, and LDS,
+//               a part of it for each wavefront, turns them into the operand, 16 bytes of one token per lane.  (Read as the operand
+//               wants them, 16 tokens side by side, a step took 2.1 us instead of 1.2: 64 places to look up per load.)
 //   O += V^T P  the result of S is 4 tokens x 1 head per lane, which is what the second product wants of P if its sum over tokens
-//               runs in that order; V comes row by row, whole rows to 16 neighbouring lanes, and in bf16 the
+//               runs in that order; V goes from memory to registers row by row, whole rows to 16 neighbouring lanes, and in bf16 the
 //               lane, which then has a few channels of the 8 tokens of its part of the sum, swaps halves of words to get 8 tokens of
-//               a channel side by side.  Neither goes through LDS.
-// Weights are bf16 for that product in two terms, p = hi + lo with an error of 2^-18: with hi alone the weights would be rounded as
+//               a channel side by side
+// The next step's keys are asked for when this one's are in LDS, its values when this one's are used up; four wavefronts of a step each in
+// flight, and two or three workgroups to a unit, keep memory busy (eight wavefronts to a workgroup were no faster, and their join slower).
+// Weights are bf16 for the second product in two terms, p = hi + lo with an error of 2^-18: with hi alone the weights would be rounded as
 // coarsely as the output, and the matrix cores have the time.
 // The maximum is raised (and what has been summed scaled down) only when a logit exceeds it by more than 8 in powers of two: p stays
 // below 256, and most steps do without an exchange between lanes.
 // Tokens behind the end, without a page or of size below 1 get z = -inf and zeros for values, whatever their rows hold.
 //
 // The four wavefronts join through LDS.  A sequence longer than a run is joined by the workgroup of its runs that ends last, which adds
-// in the order of the runs; hand-over and arrival words as in spu_tiles.hpp.
+// in the order of the runs: the parts are written past the L2 of the XCD, an arrival word per sequence and head counts the workgroups.
+// Short calls are bound by trips to memory: 4 us of the launch, then length and page, keys and values, the join's two (1 x 600 tokens: 7 us).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -42,7 +48,7 @@ template <> struct kv_piece_t<bf16_t, 4> { typedef uint32_t type __attribute__((
 template <> struct kv_piece_t<bf16_t, 2> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
 typedef int32_t kv_sizes4 __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int kMaxSplits = 256, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
+constexpr int kMaxSplits = 512, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
@@ -78,8 +84,7 @@ struct KvWork {
     int n_pages, n_heads, log2_page, D, group, chunk, tiles, cols, parts_row;      // tiles of at most `cols` query heads; parts_row: floats
     int words_each;
     int lds_words;                   // where the maxima and sums of the wavefronts lie in LDS
-    bool planned;                    // runs by the lengths
-    int fewest;                      // steps of a run, at least
+    bool planned;                    // runs by the lengths: splits is not used then, and chunk
     unsigned rows, splits, units;    // sequences x cache heads; the most runs of one; runs of all in the grid
     float* parts;                    // [runs x heads x tiles, cols, parts_row], the runs of one head of a sequence one after the other
     tile_tag_t* words;               // [rows, tiles, words_each]
@@ -91,13 +96,15 @@ struct KvWork {
 // Runs by the lengths, which every wavefront of the grid works out for itself: the steps of all sequences decide how many steps a run has,
 // one workgroup to a compute unit where the runs of up to 16 steps can be cut like that (one too many is a unit with twice the work: a few
 // longer runs are tried), two where not; a sequence's runs are of equal length.  Those of sequences with several come before the
-// sequences of one run: the long ones first.  64 sequences of 1 to 8200 tokens, 8 heads of 128, bf16: 68.5 us with runs by the bound, of
-// which 3500 in 4600 were empty and kept others waiting, 57 like this; it is a trip to memory more, 0.7 us.
-// kPlanUnits / n_parts + n runs at most, n <= 256 sequences.  Sequence 4 lane + k (or fewer to a lane) belongs to a lane.
-constexpr int kPlanUnits = 512, kPlanSeqs = 256;
+// sequences of one run: the long ones first.  Against runs by the bound on the lengths it is one more trip to memory, 0.7 us, and
+// 64 sequences of 1 to 8200 tokens, 8 heads of 128, bf16: 68.5 us by the bound (3500 of 4600 runs empty and others waiting for them), 57
+// 300 of 1 to 2000 with a bound of 32768: 313, 203.  One of 4000 with a bound of 131072: 14.6, 9.4.  One of 32768 and no other: 28.1, 26.5
+// 1000 of 100 with a bound of 4096, what it serves worst: 125, 127
+// kPlanUnits / n_parts + n runs at most, n <= 1024 sequences.  Every 64th sequence belongs to a lane.
+constexpr int kPlanUnits = 512, kPlanSeqs = 1024;
 struct RunOf { int seq, run, runs, chunk, len, before; };     // before: runs of the sequences in front
 inline __host__ __device__ int plan_runs(int n_parts) { return (kPlanUnits + n_parts - 1) / n_parts; }
-__device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, int x, int room, int step, int n_parts, int fewest, int lane)
+__device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, int x, int room, int step, int n_parts, int lane)
 {
     const int per = (n + 63) / 64;
     int len[kPlanSeqs / 64], runs[kPlanSeqs / 64];
@@ -105,7 +112,7 @@ __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, i
 #pragma unroll
     for (int k = 0; k < kPlanSeqs / 64; ++k) {
         if (k >= per) break;
-        const int i = lane * per + k;
+        const int i = 64 * k + lane;
         const int l = i < n ? lengths[i] : -1;
         len[k] = i >= n ? -1 : l < 0 ? 0 : l > room ? room : l;
         steps += (float)((len[k] + step - 1) / step);
@@ -117,7 +124,6 @@ __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, i
     const int more = each < 10 ? 1 : each / 10;
     uint32_t mine, upto, total;
     for (;; each += more) {
-        if (each < fewest) each = fewest;
         mine = 0;                                             // runs of sequences with several, sequences with one
 #pragma unroll
         for (int k = 0; k < kPlanSeqs / 64; ++k) {
@@ -144,7 +150,7 @@ __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, i
         const int here = (runs[k] > 1) == long_one ? runs[k] : 0;
         if (y >= at && y < at + here) {
             found = true;
-            r = RunOf{lane * per + k, y - at, here, 0, len[k], at + (long_one ? 0 : several)};
+            r = RunOf{64 * k + lane, y - at, here, 0, len[k], at + (long_one ? 0 : several)};
         }
         at += here;
     }
@@ -186,11 +192,11 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     if (unit >= wk.units) return;
     const int64_t held = (int64_t)a.max_pages << wk.log2_page;
     const int room = held < a.max_tokens ? (int)held : a.max_tokens;
-    // Which run of which sequence and cache head: by the bound on the lengths alone, or, where several sequences differ, by their lengths
+    // Which run of which sequence and cache head: by the lengths, or, where there is little to cut or much too much, by the bound on them
     int s, h, split, splits = 0, chunk = wk.chunk, len;
     int64_t slot;                                             // of the sequence's first run among the parts
     if (wk.planned) {
-        const RunOf r = run_by_lengths(a.lengths, a.n_seqs, unit / wk.n_heads, room, STEP, wk.n_heads * wk.tiles, wk.fewest, lane);
+        const RunOf r = run_by_lengths(a.lengths, a.n_seqs, unit / wk.n_heads, room, STEP, wk.n_heads * wk.tiles, lane);
         if (r.seq < 0) return;
         s = r.seq;
         h = unit % wk.n_heads;
@@ -604,26 +610,19 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
     }
 }
 
-// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest.  All measured, on tokens
-// that come from HBM:
+// Steps of a workgroup, of `all` that the longest sequence has, so that the estimate of the whole is smallest, where a workgroup for
+// every step would be 512 of them at most.  All measured, on tokens that come from HBM:
 //   - memory delivers 5.9 TB/s, less a share for the parts of runs that are joined and for workgroups that come and go;
-//   - a compute unit takes a step of 64 KB in 1.6 us, in 1.7 where it has two workgroups or more: one workgroup too many for the units
-//     doubles the time of some (100000 tokens, 4 heads of 128, bf16, 782 steps: 37.2 us with 196 workgroups of 16 steps, 49.1 with
-//     264 of 12, 42.3 with 392 of 8);
+//   - a compute unit takes a step of 64 KB in 1.6 us, in 1.7 where it has two workgroups or more;
 //   - joining runs takes 2.5 us and 1.2 for every further trip to memory, in groups twice that.
-// (1 x 32768 tokens, 8 heads, 256 steps: 43.6 us with 32 steps to a workgroup, 27.6 with 16, 25.8 with 12, 26.1 with 8, 26.9 with 4, 33.0 with
-// 2, 42.9 with 1; 8 x 1100, 4 heads, 9 steps: 10.2 with 1, 8.4 with 2, 10.4 with 4, 13.3 with 9.)
-// At most 8 (1024 tokens in bf16) where that leaves two workgroups to a unit: `all` is a bound, and one sequence of that length among
-// short ones would be waited for (64 sequences of 1 to 8200 tokens, 8 heads: 78 us with 16 steps, 69 with 8; 64 of 4096 lose 169 for 158).
+// (8 x 1100 tokens, 4 heads of 128, bf16, 9 steps: 10.2 us with 1, 8.4 with 2, 10.4 with 4, 13.3 with 9.)
 int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
 {
-    const int64_t fewest = std::max<int64_t>((all + kMaxSplits - 1) / kMaxSplits, (rows * tiles * all >> 22) + 1);
-    const int64_t most = rows * tiles * ((all + 7) / 8) >= 512 ? 8 : all;
     const int64_t at_once = 8 * (quads < kWaves * 64 ? kWaves * 64 / quads : 1);
     const double step_us = std::max(0.5, step_bytes / 65536.0), memory = (double)rows * all * step_bytes / 5.9e6;
-    int64_t best = std::min<int64_t>(fewest, all);
+    int best = 1;
     double least = 1e300;
-    for (int64_t n = best; n <= std::min<int64_t>(most, all); n += n < 4 ? 1 : n / 4) {
+    for (int n = 1; n <= all; n += n < 4 ? 1 : n / 4) {
         const int64_t runs = (all + n - 1) / n, each = (rows * tiles * runs + 255) / 256, even = (all + runs - 1) / runs;
         const double steps = (double)(even * each) * step_us * (each > 1 ? 1.7 : 1.6);
         double us = memory;
@@ -631,16 +630,20 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
         us = std::max(us, steps);
         if (runs > kDirect) us += 5.0 + 1.2 * (double)((kFan - 1) / at_once + (runs - 1) / kFan / at_once);
         else if (runs > 1) us += 2.5 + 1.2 * (double)((runs - 1) / at_once);
-        if (us < least) { least = us; best = even; }
+        if (us < least) { least = us; best = (int)even; }
     }
-    return (int)best;
+    return best;
 }
+
+// Steps of a run where there are more sequences than the kernel plans for: several workgroups to every unit in any case, and one of that
+// many steps is not waited for long (2000 sequences of 100 tokens with a bound of 4096: 254 us with runs of 8 steps, 178 with 32).
+constexpr int kManySteps = 32;
 
 // How a call is laid out: tiles of query heads, tokens of a run
 struct AttendPlan {
-    int dp, tiles, cols, chunk, splits, parts_row, lds_words, words_each, fewest;
+    int dp, tiles, cols, chunk, splits, parts_row, lds_words, words_each;
     bool planned;
-    int64_t rows, units, slots;
+    int64_t rows, units;
     unsigned blocks;
     size_t words, bytes, lds;
 };
@@ -654,31 +657,41 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     p.rows = (int64_t)n_seqs * n_heads;
     const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
     const int n_parts = n_heads * p.tiles;
-    p.planned = n_seqs > 1 && n_seqs <= kPlanSeqs && p.rows * p.tiles * all > 512;
-    p.fewest = (all + kMaxSplits - 1) / kMaxSplits;
+    const int64_t parts = p.rows * p.tiles;
+    p.planned = all > 1 && n_seqs <= kPlanSeqs && parts * all > kPlanUnits;
     if (p.planned) {
-        const int64_t runs = std::min<int64_t>((int64_t)n_seqs * all, plan_runs(n_parts) + n_seqs);
         p.chunk = 0;
-        p.splits = std::min<int>(kMaxSplits, std::min<int>(all, plan_runs(n_parts) + 1));
-        p.units = runs * n_heads;
-        p.slots = runs * n_parts;
+        p.splits = std::min(all, plan_runs(n_parts));
+        p.units = std::min<int64_t>((int64_t)n_seqs * all, plan_runs(n_parts) + n_seqs) * n_heads;
     } else {
-        p.chunk = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es) * step;
+        int64_t steps;
+        if (n_seqs <= kPlanSeqs) steps = attend_steps(p.rows, p.tiles, all, p.cols * ((D + 3) / 4), 2.0 * step * D * es);
+        else steps = std::max<int64_t>({kManySteps, (all + kMaxSplits - 1) / kMaxSplits, (parts * all >> 22) + 1});
+        p.chunk = (int)std::min<int64_t>(steps, all) * step;
         p.splits = (max_tokens + p.chunk - 1) / p.chunk;
         p.units = p.rows * p.splits;
-        p.slots = p.splits > 1 ? p.units * p.tiles : 0;
     }
     p.blocks = (unsigned)((p.units + 7) / 8 * 8 * p.tiles);
     p.parts_row = (D + 3) / 4 * 4 + 4;
-    p.words_each = p.splits > kDirect ? 1 + (p.splits + kFan - 1) / kFan : 1;
-    p.words = align_up((size_t)p.rows * p.tiles * p.words_each * sizeof(tile_tag_t));
-    p.bytes = p.words + align_up((size_t)p.slots * p.cols * p.parts_row * sizeof(float));
+    // Workspace for any of the layouts above that n sequences of so many tokens or fewer may get: more of either never need less
+    auto words_of = [&](int n) {
+        const int runs = n <= kPlanSeqs ? std::min(all, plan_runs(n_parts)) : std::min((all + kManySteps - 1) / kManySteps, kMaxSplits);
+        return runs > kDirect ? 1 + (runs + kFan - 1) / kFan : 1;
+    };
+    auto bytes_of = [&](int n) {
+        const int64_t each = (int64_t)n * n_parts, runs = std::min((all + kManySteps - 1) / kManySteps, kMaxSplits);
+        const int64_t slots = n > kPlanSeqs ? (runs > 1 ? std::min(each * runs, ((int64_t)1 << 22) + each) : 0) :
+                              all > 1 ? std::min<int64_t>((int64_t)n * all, plan_runs(n_parts) + n) * n_parts : 0;
+        return align_up((size_t)each * words_of(n) * sizeof(tile_tag_t)) + align_up((size_t)slots * p.cols * p.parts_row * sizeof(float));
+    };
+    p.words_each = words_of(n_seqs);
+    p.words = align_up((size_t)parts * p.words_each * sizeof(tile_tag_t));
+    p.bytes = bytes_of(n_seqs);
+    if (n_seqs > kPlanSeqs) p.bytes = std::max(p.bytes, bytes_of(kPlanSeqs));
     // keys and queries; parts of the wavefronts; partial sums over runs.  Then maxima, sums, a word
-    const size_t front = (size_t)(kWaves * (dt == LUVC_F32 ? 16 : 32) + 16) * p.dp * es + 16 * 16, parts = (size_t)kWaves * p.cols * (p.dp + 4) * sizeof(float);
+    const size_t front = (size_t)(step + 16) * p.dp * es + 16 * 16, ends = (size_t)kWaves * p.cols * (p.dp + 4) * sizeof(float);
     const size_t join = p.splits > 1 ? (size_t)kWaves * 64 * 8 * sizeof(float) : 0;
-    size_t most = front > parts ? front : parts;
-    most = most > join ? most : join;
-    p.lds_words = (int)align_up(most, 16);
+    p.lds_words = (int)align_up(std::max({front, ends, join}), 16);
     p.lds = p.lds_words + (2 * (size_t)kWaves * 16 + 4) * sizeof(float);
     return p;
 }
@@ -714,7 +727,7 @@ luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, 
     static const tile_tag_t tag = spu_next_tag();
     const double log2e = 1.4426950408889634074, full = a.scale == 0.0 ? 1.0 : std::fabs(a.scale) * log2e;
     const float scale = (float)full, rest = (float)(full - scale);
-    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, p.planned, p.fewest,
+    const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, p.planned,
                     (unsigned)p.rows, (unsigned)p.splits, (unsigned)p.units,
                     (float*)((char*)ws + p.words), (tile_tag_t*)ws, tag,
                     scale, rest, a.scale < 0.f ? -1 : a.scale > 0.f};

@@ -254,6 +254,79 @@ def test_attend_in_a_graph_follows_lengths_and_tables():
         check_attend(pool, q, out, enhance=True, lengths=lengths)
 
 
+@pytest.mark.parametrize("S, most", [(70, 80), (300, 4096), (1024, 10 ** 5), (1025, 4096), (1100, 60)])
+@pytest.mark.parametrize("dtype, Hq, H, D", [("bf16", 6, 2, 64), ("f32", 2, 2, 20)])
+def test_attend_of_many_sequences(S, most, dtype, Hq, H, D):
+    """Mostly short ones, with a long one first, last or between, and lengths of zero; the bound on them tight or far away."""
+    rng = np.random.default_rng(20 + S)
+    lengths = [int(n) for n in rng.integers(0, 40, S)]
+    for i in (0, S // 2, S - 1):
+        lengths[i] = int(rng.integers(60, 80) if most < 100 else rng.integers(1000, 3000))
+    pool = Pool(21, lengths, H, D, dtype, 16, sized=False)
+    q = pool.tensor(S, Hq, D)
+    check_attend(pool, q, lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, max_tokens=most), lengths=[min(n, most) for n in lengths])
+
+
+@pytest.mark.parametrize("lengths", [[0], [1], [17], [130], [4000], [20000]])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_of_one_sequence_within_a_distant_bound(lengths, dtype):
+    pool = Pool(22, lengths, 4, 64, dtype, 64, dead=0.2, max_pages=2048)
+    q = pool.tensor(1, 8, 64)
+    check_attend(pool, q, lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, enhance=True), enhance=True)
+
+
+@pytest.mark.parametrize("scale", [1e-300, 1e-44, -1e-20, 0.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_with_scales_next_to_zero(scale, dtype):
+    """The mean of the values of the tokens that take part."""
+    pool = Pool(23, [77, 3], 2, 64, dtype, 16, dead=0.3)
+    q = pool.tensor(2, 4, 64)
+    check_attend(pool, q, lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("D, dtype", [(33, "bf16"), (96, "f32")])
+def test_attend_strided_tensors_with_several_runs(D, dtype):
+    pool = Pool(24, [3000, 0, 1200, 40], 4, D, dtype, 16, layers=2)
+    wide = pool.tensor(4, 8 * D + 3)
+    q = wide.as_strided((4, 8, D), (wide.stride(0), D, 1), 2)
+    buf = torch.full((4, 8 * D + 5), 7.0, dtype=TORCH[dtype], device="cuda")
+    out = buf.as_strided((4, 8, D), (buf.stride(0), D, 1), 3)
+    lv.luvc_kv_attend(pool.cache, 1, q, pool.tt, pool.lt, max_tokens=10 ** 5, out=out)
+    check_attend(pool, q.contiguous(), out.contiguous(), layer=1)
+    assert bool((buf[:, :3] == 7).all()) and bool((buf[:, 3 + 8 * D:] == 7).all())
+
+
+def test_attend_graphs_with_room_to_grow_on_one_workspace():
+    """Captured for more tokens than the sequences have yet; a graph of four sequences, one of a single one and eager calls of three take
+    turns on a workspace that was made for the largest of them."""
+    most = 8192
+    pool = Pool(25, [6000, 900, 40, 1], 4, 64, "bf16", 16, max_pages=most // 16)
+    q = pool.tensor(4, 8, 64)
+    outs = [torch.zeros((n, 8, 64), dtype=torch.bfloat16, device="cuda") for n in (4, 1)]
+    ws = torch.empty(lv.luvc_kv_attend_workspace_bytes(pool.cache, 4, 8, most), dtype=torch.uint8, device="cuda")
+    run = lambda o: lv.luvc_kv_attend(pool.cache, 0, q[:len(o)], pool.tt[:len(o)], pool.lt[:len(o)], max_tokens=most, enhance=True, workspace=ws, out=o)
+    for o in outs:
+        run(o)
+    torch.cuda.synchronize()
+    graphs = []
+    for o in outs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(o)
+    for lengths in ([6000, 900, 40, 1], [5999, 0, 40, 0], [1, 700, 3, 1], [0, 0, 0, 0], [2500, 899, 39, 1]):
+        pool.lt.copy_(torch.tensor(lengths, dtype=torch.int32))
+        q.normal_()
+        for o in outs:
+            o.fill_(5.0)
+        graphs[0].replay()
+        three = run(torch.empty_like(q[:3]))
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        check_attend(pool, q, outs[0], enhance=True, lengths=lengths)
+        check_attend(pool, q[:3], three, enhance=True, lengths=lengths[:3], table=pool.table[:3])
+        check_attend(pool, q[:1], outs[1], enhance=True, lengths=lengths[:1], table=pool.table[:1])
+
+
 # ------------------------------------------------------------------ moving rows
 
 def bits(t):

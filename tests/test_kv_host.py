@@ -94,6 +94,26 @@ def test_attend_refusals_and_workspace(L):
     assert L.luvc_kv_attend_workspace_bytes(None, 2, 8, 64) == 0
 
 
+@pytest.mark.parametrize("hq, h, D, dtype", [(32, 8, 128, lv.LUVC_BF16), (28, 4, 128, lv.LUVC_BF16), (4, 1, 64, lv.LUVC_F32), (64, 64, 96, lv.LUVC_BF16), (40, 1, 256, lv.LUVC_F32),
+                                             (1024, 1024, 8, lv.LUVC_BF16)])
+def test_a_workspace_serves_fewer_sequences_and_shorter_ones(L, hq, h, D, dtype):
+    c = cache(n_heads=h, D=D, dtype=dtype)
+    seqs = [1, 2, 3, 7, 8, 16, 60, 64, 65, 128, 255, 256, 257, 500, 1023, 1024, 1025, 1100, 2048, 4000]
+    tokens = [1, 16, 63, 64, 65, 127, 128, 129, 300, 512, 513, 1000, 2048, 4096, 4097, 5000, 8200, 30000, 65537, 10 ** 5, 10 ** 6, 2 ** 30 - 1]
+    need = [[L.luvc_kv_attend_workspace_bytes(ctypes.byref(c), n, hq, t) for t in tokens] for n in seqs]
+    for a, b in zip(need, need[1:]):
+        assert all(0 < x <= y for x, y in zip(a, b) if y)   # 0: too many sequences
+    for row in need:
+        assert all(x <= y for x, y in zip(row, row[1:]))
+
+
+def test_attend_refuses_scales_beyond_fp32(L):
+    for v in (3e38, -3e38, 1e39, float("inf"), float("-inf")):
+        s = ctypes.c_double(v)
+        assert L.luvc_kv_attend(ctypes.byref(cache()), 0, FAKE, 512, 8, 2, FAKE, 4, FAKE, 64, ctypes.byref(s), 0, FAKE, 512, None, 0, None) == lv.LUVC_ERR_INVALID_ARG
+        assert "scale" in lv.last_error()
+
+
 def test_compact_refusals(L):
     c = cache()
     def call(lengths, first, span, keep, kept=FAKE, mi=4, mo=4, tin=FAKE, tout=FAKE):
