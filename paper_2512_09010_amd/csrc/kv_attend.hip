@@ -46,7 +46,6 @@ template <typename T, int W> struct kv_piece_t;
 template <> struct kv_piece_t<float, 4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
 template <> struct kv_piece_t<bf16_t, 4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
 template <> struct kv_piece_t<bf16_t, 2> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
-typedef int32_t kv_sizes4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kMaxSplits = 512, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
 constexpr float kLn2 = 0.69314718055994530942f;
