@@ -47,7 +47,7 @@ template <> struct kv_piece_t<float, 4> { typedef uint32_t type __attribute__((e
 template <> struct kv_piece_t<bf16_t, 4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
 template <> struct kv_piece_t<bf16_t, 2> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
 
-constexpr int kMaxSplits = 512, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
+constexpr int kMaxSplits = 768, kDirect = 32, kFan = 16;      // runs of a sequence: at most, joined at once at most, else in groups of
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.0e38f;              // the maximum of nothing: finite, so that differences to it are no NaN
 
@@ -92,17 +92,20 @@ struct KvWork {
     int sign;                        // of the queries: -1, 0 (as if they were zero), 1
 };
 
-// Runs by the lengths, which every wavefront of the grid works out for itself: the steps of all sequences decide how many steps a run has,
-// one workgroup to a compute unit where the runs of up to 16 steps can be cut like that (one too many is a unit with twice the work: a few
-// longer runs are tried), two where not; a sequence's runs are of equal length.  Those of sequences with several come before the
-// sequences of one run: the long ones first.  Against runs by the bound on the lengths it is one more trip to memory, 0.7 us, and
-// 64 sequences of 1 to 8200 tokens, 8 heads of 128, bf16: 68.5 us by the bound (3500 of 4600 runs empty and others waiting for them), 57
-// 300 of 1 to 2000 with a bound of 32768: 313, 203.  One of 4000 with a bound of 131072: 14.6, 9.4.  One of 32768 and no other: 28.1, 26.5
-// 1000 of 100 with a bound of 4096, what it serves worst: 125, 127
-// kPlanUnits / n_parts + n runs at most, n <= 1024 sequences.  Every 64th sequence belongs to a lane.
-constexpr int kPlanUnits = 512, kPlanSeqs = 1024;
+// Runs by the lengths, which every wavefront of the grid works out for itself: the steps of all sequences decide how many steps a run has.
+// Cut for one workgroup to a compute unit where that makes runs of up to 16 steps, else for two, else for three: one too many is a
+// unit with twice the work, so a few longer runs are tried before it goes on to the finer cut, which is kept however many come out.  A
+// sequence's runs are of equal length.  Those of sequences with several come before the sequences of one run: the long ones first.
+// Sequences of 1 to 32768 tokens, 16 of them, 4 heads of 128, bf16: 107 us without the third cut (544 runs for 512 places), 93 with it;
+// 16 of 4096 in fp32, which fit two to a unit: 54 cut for three, 47 for two; five to a unit are no better, and 128 of 1024 take 50 for 43.
+// Against runs by the bound on the lengths it is one more trip to memory, 0.7 us, and
+//   64 sequences of 1 to 8200 tokens, 8 heads: 68.5 us by the bound (3500 of 4600 runs empty and others waiting for them), 57
+//   300 of 1 to 2000 with a bound of 32768: 313, 202.  One of 4000 with a bound of 131072: 14.6, 9.4.  One of 32768 and no other: 28.1, 26.6
+//   1000 of 100 with a bound of 4096, what it serves worst: 125, 130
+// kFinest * kUnits / n_parts + n runs at most, n <= 1024 sequences.  Every 64th sequence belongs to a lane.
+constexpr int kUnits = 256, kFinest = 3, kPlanSeqs = 1024;
 struct RunOf { int seq, run, runs, chunk, len, before; };     // before: runs of the sequences in front
-inline __host__ __device__ int plan_runs(int n_parts) { return (kPlanUnits + n_parts - 1) / n_parts; }
+inline __host__ __device__ int plan_runs(int n_parts) { return (kFinest * kUnits + n_parts - 1) / n_parts; }
 __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, int x, int room, int step, int n_parts, int lane)
 {
     const int per = (n + 63) / 64;
@@ -118,11 +121,13 @@ __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, i
     }
     // no rounding of the sum may make it smaller than it is: the runs have to fit the grid
     steps = wave_sum(steps) * 1.0001f;
-    const float one = steps * (float)n_parts / (kPlanUnits / 2), two = steps / (float)plan_runs(n_parts);
-    int each = (int)ceilf(one <= 16.f ? one : two), left = one <= 16.f ? 3 : 0;
-    const int more = each < 10 ? 1 : each / 10;
+    // workgroups to a unit that the runs are cut for; more than kUnits of each have no chance where there are more sequences
+    const float one = steps * (float)n_parts / kUnits;
+    int fine = n * n_parts > 2 * kUnits ? kFinest : one <= 16.f && n * n_parts <= kUnits ? 1 : 2, tries = 3;
+    auto cut = [&]() { return (int)ceilf(fine == kFinest ? steps / (float)plan_runs(n_parts) : fine == 1 ? one : one * 0.5f); };
+    int each = cut();
     uint32_t mine, upto, total;
-    for (;; each += more) {
+    for (;;) {
         mine = 0;                                             // runs of sequences with several, sequences with one
 #pragma unroll
         for (int k = 0; k < kPlanSeqs / 64; ++k) {
@@ -133,8 +138,14 @@ __device__ __forceinline__ RunOf run_by_lengths(const int32_t* lengths, int n, i
         }
         upto = wave_scan_incl(mine);
         total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-        if (left == 0 || ((total >> 16) + (total & 0xffffu)) * n_parts <= kPlanUnits / 2) break;
-        if (--left == 0) each = (int)ceilf(two) - more;
+        if (fine == kFinest || (int)((total >> 16) + (total & 0xffffu)) * n_parts <= fine * kUnits) break;
+        if (--tries) {
+            each += each < 10 ? 1 : each / 10;
+        } else {
+            ++fine;
+            tries = 3;
+            each = cut();
+        }
     }
     const int several = (int)(total >> 16);
     RunOf r{-1, 0, 0, 0, 0, 0};
@@ -657,7 +668,7 @@ AttendPlan attend_plan(int n_seqs, int n_q_heads, int n_heads, int D, luvc_dtype
     const int step = kWaves * (dt == LUVC_F32 ? 16 : 32), all = (max_tokens + step - 1) / step;
     const int n_parts = n_heads * p.tiles;
     const int64_t parts = p.rows * p.tiles;
-    p.planned = all > 1 && n_seqs <= kPlanSeqs && parts * all > kPlanUnits;
+    p.planned = all > 1 && n_seqs <= kPlanSeqs && parts * all > 2 * kUnits;
     if (p.planned) {
         p.chunk = 0;
         p.splits = std::min(all, plan_runs(n_parts));
