@@ -36,7 +36,7 @@ def parse():
     ap.add_argument("--oim-wide", action="store_true",
                     help="also time luvc_oim_merge_wide on the workload's grid in the paper's setting (whole-line matching, merge number 2, three operations)")
     ap.add_argument("--next-rows", action="store_true",
-                    help="also time the calls beyond the hot path: keyed merge, value enhancement, a cascade, ragged batches")
+                    help="also time the calls beyond the hot path: keyed merge, value enhancement, a cascade, ragged batches, the cache")
     ap.add_argument("--rotate-mb", type=float, default=600.0, help="distinct input bytes cycled through (defeats cache reuse)")
     ap.add_argument("--preheat-ms", type=float, default=100.0, help="untimed steps run for this long before the warm-up steps, to bring the clocks up (0: none)")
     return ap.parse_args()
@@ -524,6 +524,43 @@ def next_rows_leg(lv, torch, w, xs_oim, xs_spu, n_rot, tdt, code, es, stream, st
         ms, kern = _time_call(torch, lv, lambda i: lv.luvc_spu_stage_ragged(xp[i % 2], lengths, sg, kp, stream=stream), steps)
         res["spu_ragged"] = {"what": f"luvc_spu_stage_ragged, lengths {lengths} (the binding allocates the outputs on every call)",
                              "ms_per_call": round(ms, 5), "kernels": kern}
+
+    # ---- the cache of the layers in front of a stage: the samples' tokens with 64 of text around them are written, pruned as the cascade's first
+    # stage left them, decoded over and forked; 2 layers, 16 query heads on 4 of 128, pages of 64 tokens
+    heads, q_heads, Dh, P, layers, text, kids = 4, 16, 128, 64, 2, 64, 4
+    n0, n1 = N + text, keeps[0] + text
+    w0, w1 = -(-n0 // P), -(-(n1 + 1) // P)
+    n_pages = Bs * (w0 + w1) + kids
+    k, v = (torch.zeros((layers, n_pages, heads, P, Dh), dtype=tdt, device=dev) for _ in range(2))
+    cache = lv.KvCache(k, v, torch.ones((n_pages, P), dtype=torch.int32, device=dev))
+    refs = torch.zeros(n_pages, dtype=torch.int32)
+    before = torch.stack([lv.luvc_kv_take(refs, w0) for _ in range(Bs)])
+    after = torch.stack([lv.luvc_kv_take(refs, w1) for _ in range(Bs)])
+    t0, t1 = before.to(dev), after.to(dev)
+    qkv = torch.randn((Bs * n0, q_heads + 2 * heads, Dh), device=dev).to(tdt)
+    seq = torch.arange(Bs, dtype=torch.int32, device=dev).repeat_interleave(n0)
+    pos = torch.arange(n0, dtype=torch.int32, device=dev).repeat(Bs)
+    ms, kern = _time_call(torch, lv, lambda i: lv.luvc_kv_write(cache, i % layers, qkv[:, q_heads:q_heads + heads], qkv[:, q_heads + heads:], pos, t0, seq=seq, stream=stream), steps)
+    res["kv_write"] = {"what": f"luvc_kv_write, {Bs} prompts of {n0} tokens, one layer", "ms_per_call": round(ms, 5), "kernels": kern}
+    kept = outs[0]["kept_idx"].reshape(-1)
+    ms, kern = _time_call(torch, lv, lambda i: lv.luvc_kv_compact(cache, kept, [n0] * Bs, [text // 2] * Bs, [N] * Bs, [keeps[0]] * Bs, t0, t1, stream=stream), steps)
+    res["kv_compact"] = {"what": f"luvc_kv_compact, {Bs} sequences of {n0} tokens to {n1}, {layers} layers", "ms_per_call": round(ms, 5), "kernels": kern}
+    now = torch.full((Bs,), n1 + 1, dtype=torch.int32, device=dev)
+    wsa = torch.empty(lv.luvc_kv_attend_workspace_bytes(cache, Bs, q_heads, w1 * P), dtype=torch.uint8, device=dev)
+    att = torch.empty((Bs, q_heads, Dh), dtype=tdt, device=dev)
+    last = now - 1
+
+    def decode(i):
+        new = qkv[i % 2 * Bs:i % 2 * Bs + Bs]
+        lv.luvc_kv_write(cache, i % layers, new[:, q_heads:q_heads + heads], new[:, q_heads + heads:], last, t1, stream=stream)
+        lv.luvc_kv_attend(cache, i % layers, new[:, :q_heads], t1, now, max_tokens=w1 * P, enhance=True, workspace=wsa, stream=stream, out=att)
+    ms, kern = _time_call(torch, lv, decode, steps)
+    res["kv_decode"] = {"what": f"luvc_kv_write + luvc_kv_attend of one token of {Bs} sequences over {n1 + 1}, one layer", "ms_per_call": round(ms, 5), "kernels": kern}
+
+    def fork(i):
+        lv.luvc_kv_release(refs, lv.luvc_kv_fork(cache, refs, after[0], n1 + 1, kids, stream=stream))
+    ms, kern = _time_call(torch, lv, fork, steps)
+    res["kv_fork"] = {"what": f"luvc_kv_fork of {n1 + 1} tokens into {kids} + luvc_kv_release, {layers} layers", "ms_per_call": round(ms, 5), "kernels": kern}
     return res
 
 
