@@ -624,7 +624,8 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 // every step would be 512 of them at most.  All measured, on tokens that come from HBM:
 //   - memory delivers 5.9 TB/s, less a share for the parts of runs that are joined and for workgroups that come and go;
 //   - a compute unit takes a step of 64 KB in 1.6 us, in 1.7 where it has two workgroups or more;
-//   - joining runs takes 2.5 us and 1.2 for every further trip to memory, in groups twice that.
+//   - joining runs takes 3.3 us and 1.2 for every further trip to memory, in groups 5.8 (8 x 300 tokens, 4 heads, 3 steps: 7.0 us with one
+//     run, 7.4 with three; 1 x 600, 5 steps: 8.4, 6.7 with five).
 // (8 x 1100 tokens, 4 heads of 128, bf16, 9 steps: 10.2 us with 1, 8.4 with 2, 10.4 with 4, 13.3 with 9.)
 int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
 {
@@ -638,8 +639,8 @@ int attend_steps(int64_t rows, int tiles, int all, int quads, double step_bytes)
         double us = memory;
         if (runs > 1) us *= 1.0 + 0.25 / std::sqrt((double)even);
         us = std::max(us, steps);
-        if (runs > kDirect) us += 5.0 + 1.2 * (double)((kFan - 1) / at_once + (runs - 1) / kFan / at_once);
-        else if (runs > 1) us += 2.5 + 1.2 * (double)((runs - 1) / at_once);
+        if (runs > kDirect) us += 5.8 + 1.2 * (double)((kFan - 1) / at_once + (runs - 1) / kFan / at_once);
+        else if (runs > 1) us += 3.3 + 1.2 * (double)((runs - 1) / at_once);
         if (us < least) { least = us; best = (int)even; }
     }
     return best;
