@@ -402,8 +402,9 @@ luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q,
  *               luvc_spu_stage and luvc_spu_stage_ragged return.  One outside 0..span[i]-1 moves nothing
  *   table_in    device [n_seqs, max_pages_in]: where the tokens are
  *   table_out   device [n_seqs, max_pages_out]: where they go; lengths[i] - span[i] + n_keep[i] tokens
- * Pages of table_out must not be read by the call (from any of its sequences), with one exception: a page of tokens that stay
- * where they are, so that first[i] / page_tokens pages of either table's row may be the same.
+ * Pages of table_out must not be read by the call (from any of its sequences) and belong to one sequence each, with one exception:
+ * pages of tokens that stay where they are, so that the first first[i] / page_tokens pages of either table's row may be the same
+ * (and those of several sequences, which share a prompt).  Pages of table_in may be read by any number of sequences.
  * The host arrays are used up when the call returns.  A call of more than 64 sequences is several launches.
  * Limits: sequences of fewer than 2^25 tokens.
  */

@@ -480,6 +480,86 @@ def test_fork(dtype, D, P, H, length, children):
     assert torch.equal(refs, start)
 
 
+def test_compact_of_forks_that_share_a_prompt():
+    """Three sequences read the same pages; two of them leave the pages of the front where they are, for both."""
+    P, H, D, n, first, span = 16, 2, 64, 100, 35, 50
+    pool = Pool(26, [n], H, D, "bf16", P, layers=2, extra=20)
+    table = np.tile(pool.table[0], (3, 1))
+    kept = np.concatenate([np.sort(np.random.default_rng(27 + i).permutation(span)[:k]) for i, k in enumerate((10, 0, 50))]).astype(np.int32)
+    out = np.full((3, 7), -1, np.int32)
+    for i, after in enumerate((60, 50, 100)):
+        for j in range(-(-after // P)):
+            out[i, j] = table[i, j] if i < 2 and j < first // P else pool.free.pop()
+    k, v, sizes = bits(pool.kt).copy(), bits(pool.vt).copy(), pool.sizes.copy()
+    want = ref.compact([k, v], sizes, kept, [n] * 3, [first] * 3, [span] * 3, [10, 0, 50], table, out)
+    assert lv.luvc_kv_compact(pool.cache, torch.tensor(kept).cuda(), [n] * 3, [first] * 3, [span] * 3, [10, 0, 50], torch.tensor(table).cuda(), torch.tensor(out).cuda()) == want
+    assert np.array_equal(bits(pool.kt), k) and np.array_equal(bits(pool.vt), v) and np.array_equal(pool.st.cpu().numpy(), sizes)
+
+
+def test_captured_writes_copies_and_compactions():
+    """The host lists of a captured call are those of the capture, whatever becomes of them; device arrays are read anew."""
+    P, H, D, n = 16, 2, 80, 150
+    pool = Pool(28, [n, n], H, D, "bf16", P, layers=2, extra=40)
+    nk, nv = pool.tensor(6, H, D), pool.tensor(6, H, D)
+    seq, pos = torch.tensor([0, 1, 0, 1, -1, 0], dtype=torch.int32).cuda(), torch.tensor([3, 149, 77, 0, 5, 16], dtype=torch.int32).cuda()
+    kept = torch.arange(24, dtype=torch.int32).cuda()
+    out = torch.tensor([[pool.free.pop() for _ in range(10)] for _ in range(2)], dtype=torch.int32).cuda()
+    src, dst = torch.tensor(pool.table[0, :3]), torch.tensor([pool.free.pop() for _ in range(3)], dtype=torch.int32)
+    spans = [torch.tensor(x, dtype=torch.int32) for x in ([n, n], [20, 0], [100, 140], [12, 12])]
+
+    def run(spans, src, dst):
+        lv.luvc_kv_write(pool.cache, 1, nk, nv, pos, pool.tt, seq=seq)
+        lv.luvc_kv_compact(pool.cache, kept, *spans, pool.tt, out)
+        lv.luvc_kv_copy_pages(pool.cache, src, dst)
+    held = [list(map(int, t)) for t in spans], list(map(int, src)), list(map(int, dst))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        run(spans, src, dst)
+    for t in (*spans, src, dst):
+        t.fill_(0)
+    start = pool.kt.clone(), pool.vt.clone(), pool.st.clone()
+    for step in range(4):
+        nk.normal_()
+        pos[0] = 4 + step
+        kept.copy_(torch.cat([torch.randperm(100)[:12].sort().values, torch.randperm(140)[:12].sort().values]).to(torch.int32))
+        after = []
+        for f in (graph.replay, lambda: run(*held)):
+            for t, was in zip((pool.kt, pool.vt, pool.st), start):
+                t.copy_(was)
+            f()
+            torch.cuda.synchronize()
+            after.append((bits(pool.kt).copy(), bits(pool.vt).copy(), pool.st.cpu().numpy().copy()))
+        assert all(np.array_equal(a, b) for a, b in zip(*after))
+        assert not np.array_equal(after[0][0], bits(start[0]))
+
+
+def test_calls_the_binding_refuses():
+    pool = Pool(29, [40, 20], 2, 64, "bf16", 16)
+    c, q, n = pool.cache, pool.tensor(2, 4, 64), pool.tensor(2, 2, 64)
+    pos = pool.lt - 1
+    before = bits(pool.kt).copy(), pool.st.clone()
+    for bad in (lambda: lv.luvc_kv_attend(c, 0, q.float(), pool.tt, pool.lt), lambda: lv.luvc_kv_attend(c, 0, q.cpu(), pool.tt, pool.lt),
+                lambda: lv.luvc_kv_attend(c, 0, q, pool.tt.cpu(), pool.lt), lambda: lv.luvc_kv_attend(c, 0, q, pool.tt, pool.lt.long()),
+                lambda: lv.luvc_kv_attend(c, 0, q, pool.tt[:1], pool.lt), lambda: lv.luvc_kv_attend(c, 0, q.transpose(1, 2), pool.tt, pool.lt),
+                lambda: lv.luvc_kv_attend(c, 0, q[:, :3], pool.tt, pool.lt), lambda: lv.luvc_kv_attend(c, 1, q, pool.tt, pool.lt),
+                lambda: lv.luvc_kv_attend(c, 0, q, pool.tt, pool.lt, workspace=torch.empty(0, dtype=torch.uint8, device="cuda")),
+                lambda: lv.luvc_kv_attend(c, 0, q, pool.tt, pool.lt, out=torch.empty(1, 4, 64, dtype=torch.bfloat16, device="cuda").expand(2, 4, 64)),
+                lambda: lv.luvc_kv_attend(lv.KvCache(pool.kt, pool.vt), 0, q, pool.tt, pool.lt, enhance=True),
+                lambda: lv.luvc_kv_write(c, 0, n, n[:1], pos, pool.tt), lambda: lv.luvc_kv_write(c, 0, n.cpu(), n.cpu(), pos, pool.tt),
+                lambda: lv.luvc_kv_write(c, 0, n, n, pos[:1], pool.tt), lambda: lv.luvc_kv_write(c, -1, n, n, pos, pool.tt),
+                lambda: lv.luvc_kv_write(lv.KvCache(pool.kt, pool.vt), 0, n, n, pos, pool.tt, sizes=pos),
+                lambda: lv.luvc_kv_copy_pages(c, [0, 1], [2]), lambda: lv.luvc_kv_copy_pages(c, [0], [0]), lambda: lv.luvc_kv_copy_pages(c, [0], [pool.n_pages]),
+                lambda: lv.luvc_kv_compact(c, pos, [40, 20], [0, 0], [30, 10], [1, 0], pool.tt, pool.tt),
+                lambda: lv.luvc_kv_compact(c, pos, [40, 20], [0, 0], [30, 10], [1], pool.tt, pool.tt),
+                lambda: lv.luvc_kv_fork(c, torch.ones(3, dtype=torch.int32), [0], 5, 1), lambda: lv.luvc_kv_fork(c, torch.ones(pool.n_pages, dtype=torch.int64), [0], 5, 1),
+                lambda: lv.KvCache(pool.kt.cpu(), pool.vt.cpu()), lambda: lv.KvCache(pool.kt, pool.vt.float()), lambda: lv.KvCache(pool.kt, pool.vt, pool.st[:1])):
+        with pytest.raises((AssertionError, lv.LuvcError)):
+            bad()
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(pool.kt), before[0]) and torch.equal(pool.st, before[1])
+
+
 # ------------------------------------------------------------------ all of it, as a serving program uses it
 
 @pytest.mark.parametrize("dtype, model, H, Hq, D", [("bf16", 512, 2, 8, 64), ("f32", 256, 2, 2, 128)])
