@@ -25,10 +25,10 @@ luvc_status kv_write_run(const luvc_kv_cache& c, int layer, const void* k, int64
 // rows [0, rows) of page src[i * src_step] to page dst[i * dst_step], all layers, i < n
 luvc_status kv_copy_run(const luvc_kv_cache& c, const int32_t* src, int src_step, const int32_t* dst, int dst_step, int n, int rows, hipStream_t st);
 
-constexpr int kKvMaxSeqs = 64;                   // sequences of a compacting launch
 struct KvSpan { int32_t first, span, keep, after; int64_t kept; };       // kept: where its entries of kept_idx start
-struct KvSpans { int32_t n, row0; KvSpan s[kKvMaxSeqs]; };               // row0: table row of the first one
-luvc_status kv_compact_run(const luvc_kv_cache& c, const KvSpans& spans, const int32_t* kept_idx, const int32_t* table_in, int max_in,
+constexpr int kKvMaxSeqs = 64;                   // sequences of a call
+// spans[i] is table row row0 + i, i < n
+luvc_status kv_compact_run(const luvc_kv_cache& c, const KvSpan* spans, int n, int row0, const int32_t* kept_idx, const int32_t* table_in, int max_in,
                            const int32_t* table_out, int max_out, hipStream_t st);
 
 struct KvAttend {

@@ -152,15 +152,14 @@ luvc_status luvc_kv_compact(const luvc_kv_cache* cache, int n_seqs, const int32_
     if (kept && !kept_idx) { set_error("kept_idx must not be NULL"); return LUVC_ERR_INVALID_ARG; }
     kept = 0;
     for (int i0 = 0; i0 < n_seqs; i0 += kKvMaxSeqs) {
-        KvSpans spans;
-        spans.n = n_seqs - i0 < kKvMaxSeqs ? n_seqs - i0 : kKvMaxSeqs;
-        spans.row0 = i0;
-        for (int j = 0; j < spans.n; ++j) {
+        KvSpan spans[kKvMaxSeqs];
+        const int n = n_seqs - i0 < kKvMaxSeqs ? n_seqs - i0 : kKvMaxSeqs;
+        for (int j = 0; j < n; ++j) {
             const int i = i0 + j;
-            spans.s[j] = KvSpan{first[i], span[i], n_keep[i], lengths[i] - span[i] + n_keep[i], kept};
+            spans[j] = KvSpan{first[i], span[i], n_keep[i], lengths[i] - span[i] + n_keep[i], kept};
             kept += n_keep[i];
         }
-        rc = kv_compact_run(*cache, spans, kept_idx, table_in, max_pages_in, table_out, max_pages_out, (hipStream_t)hip_stream);
+        rc = kv_compact_run(*cache, spans, n, i0, kept_idx, table_in, max_pages_in, table_out, max_pages_out, (hipStream_t)hip_stream);
         if (rc != LUVC_OK) return rc;
     }
     return LUVC_OK;
