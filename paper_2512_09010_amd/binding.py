@@ -669,6 +669,8 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
     if workspace is None:
         need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
         workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
+        if stream is not None:                         # it is freed on return, before another stream may have come to the call
+            workspace.record_stream(stream)
     if out is None:
         out = nat.torch.empty(shape, dtype=dtype, device=q.device)
     assert out.shape == shape and out.dtype is dtype

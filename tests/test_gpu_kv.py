@@ -224,6 +224,25 @@ def test_attend_with_stale_workspaces_streams_and_repeats(long):
             assert torch.equal(t, again)
 
 
+def test_attend_on_another_stream_keeps_its_own_workspace():
+    """A workspace that the binding allocates is not handed out again before the call on the other stream has ended."""
+    pool = Pool(30, [3000, 1, 700], 2, 128, "bf16", 16)
+    q, out = pool.tensor(3, 8, 128), torch.zeros((3, 8, 128), dtype=torch.bfloat16, device="cuda")
+    need = lv.luvc_kv_attend_workspace_bytes(pool.cache, 3, 8, 16 * pool.width)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    want = lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt)             # leaves one free block of that size
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                      # holds the call back while its workspace might be handed out
+    lv.luvc_kv_attend(pool.cache, 0, q, pool.tt, pool.lt, stream=side, out=out)
+    noise = [torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(16)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    assert all(bool((t == 255).all()) for t in noise)
+
+
 def test_attend_in_a_graph_follows_lengths_and_tables():
     pool = Pool(8, [2000, 900, 40, 1], 2, 64, "bf16", 16)
     q, out = pool.tensor(4, 4, 64), torch.zeros((4, 4, 64), dtype=torch.bfloat16, device="cuda")
