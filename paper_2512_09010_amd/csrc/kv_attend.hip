@@ -572,45 +572,67 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         }
         __syncthreads();
         if (!last_flag) return;
-        constexpr int AHEAD = 8;                              // runs of a thread in flight
-        for (int i0 = 0; i0 < nh * QUADS; i0 += NT) {
-            const int i = i0 + item0, col = i / QUADS, d = i % QUADS * 4;
-            const bool in = col < nh && d < D;
-            const uint32_t at = (uint32_t)((first * part + (in ? col * wk.parts_row : 0)) * 4);
-            Sum t{kLowest, 0.f, {}};
+        // AHEAD runs of a thread in flight, of one set of four channels or of several where there are more than threads
+        auto join = [&](auto SETS, int i0) {
+            constexpr int S = decltype(SETS)::value, AHEAD = 8;
+            int col[S], d[S];
+            bool in[S];
+            uint32_t at[S];
+            Sum t[S];
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                const int i = i0 + j * NT + item0;
+                col[j] = i / QUADS;
+                d[j] = i % QUADS * 4;
+                in[j] = col[j] < nh && d[j] < D;
+                at[j] = (uint32_t)((first * part + (in[j] ? col[j] * wk.parts_row : 0)) * 4);
+                t[j] = Sum{kLowest, 0.f, {}};
+            }
 #pragma unroll 1
             for (int k0 = grp; k0 < runs; k0 += AHEAD * groups) {
-                tile_vec<4>::type x[AHEAD];
-                tile_vec<2>::type ml[AHEAD];
+                tile_vec<4>::type x[S][AHEAD];
+                tile_vec<2>::type ml[S][AHEAD];
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
                     const int run = k0 + k * groups;
-                    const uint32_t from = (uint32_t)((run < runs ? run : runs - 1) * apart * part * 4) + at;
-                    x[k] = tile_vec<4>::load(all, from + (in ? d * 4 : 0));
-                    ml[k] = tile_vec<2>::load(all, from + (wk.parts_row - 4) * 4);
+                    const uint32_t from = (uint32_t)((run < runs ? run : runs - 1) * apart * part * 4);
+#pragma unroll
+                    for (int j = 0; j < S; ++j) {
+                        x[j][k] = tile_vec<4>::load(all, from + at[j] + (in[j] ? d[j] * 4 : 0));
+                        ml[j][k] = tile_vec<2>::load(all, from + at[j] + (wk.parts_row - 4) * 4);
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
                     const bool there = k0 + k * groups < runs;
-                    t.add(there ? __uint_as_float(ml[k][0]) : kLowest, there ? __uint_as_float(ml[k][1]) : 0.f, there ? __builtin_bit_cast(kv_f32x4, x[k]) : kv_f32x4{});
+#pragma unroll
+                    for (int j = 0; j < S; ++j)
+                        t[j].add(there ? __uint_as_float(ml[j][k][0]) : kLowest, there ? __uint_as_float(ml[j][k][1]) : 0.f, there ? __builtin_bit_cast(kv_f32x4, x[j][k]) : kv_f32x4{});
                 }
             }
-            if (groups > 1) {                                 // nh * QUADS < NT: one round
+            if (S == 1 && groups > 1) {                       // nh * QUADS < NT: one round
                 float* red = so + tid * 8;
-                *(kv_f32x4*)red = t.v;
-                red[4] = t.top;
-                red[5] = t.sum;
+                *(kv_f32x4*)red = t[0].v;
+                red[4] = t[0].top;
+                red[5] = t[0].sum;
                 __syncthreads();
 #pragma unroll 1
                 for (int k = 1; grp == 0 && k < groups; ++k) {
                     red += 8 << log2_items;
-                    t.add(red[4], red[5], *(const kv_f32x4*)red);
+                    t[0].add(red[4], red[5], *(const kv_f32x4*)red);
                 }
             }
-            if (!in || grp) continue;
-            if (done) store(col, d, t.mean());
-            else keep(first, col, d, t);
-        }
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                if (!in[j] || grp) continue;
+                if (done) store(col[j], d[j], t[j].mean());
+                else keep(first, col[j], d[j], t[j]);
+            }
+        };
+        constexpr int SETS = DP / 64;                         // of 16 heads
+        if (nh * QUADS <= NT) join(std::integral_constant<int, 1>{}, 0);
+        else if (nh * QUADS <= 2 * NT) join(std::integral_constant<int, SETS < 2 ? 1 : 2>{}, 0);
+        else join(std::integral_constant<int, SETS>{}, 0);
         if (done) return;
         // the groups' sums are in the places of their first runs
         first = 0;
