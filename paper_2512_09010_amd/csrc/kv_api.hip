@@ -57,9 +57,16 @@ bool layer_ok(const luvc_kv_cache* c, int layer, luvc_status* rc)
 // The n free pages with the lowest numbers go to pages[0], pages[step], ...; false if there are fewer
 bool take(int32_t* refs, int n_pages, int n, int32_t* pages, int64_t step)
 {
+    constexpr int AT_ONCE = 16;                      // pages in use are passed over in groups: a full pool is a long list
     int got = 0;
-    for (int p = 0; p < n_pages && got < n; ++p)
+    for (int p = 0; p < n_pages && got < n; ++p) {
+        if (p % AT_ONCE == 0 && p + AT_ONCE <= n_pages) {
+            int free_ones = 0;
+            for (int i = 0; i < AT_ONCE; ++i) free_ones += refs[p + i] == 0;
+            if (!free_ones) { p += AT_ONCE - 1; continue; }
+        }
         if (refs[p] == 0) pages[got++ * step] = p;
+    }
     if (got < n) { set_error("%d pages are needed, %d of %d are free", n, got, n_pages); return false; }
     for (int i = 0; i < n; ++i) refs[pages[i * step]] = 1;
     return true;
@@ -177,16 +184,22 @@ luvc_status luvc_kv_copy_pages(const luvc_kv_cache* cache, const int32_t* src, c
             set_error("pair %d: pages %d and %d are not in 0..%d", i, src[i], dst[i], cache->n_pages - 1);
             return LUVC_ERR_INVALID_ARG;
         }
-    // a page is written once and never read: a bit per page that is read, one per page that is written
-    unsigned char* seen = (unsigned char*)calloc((size_t)cache->n_pages, 1);
-    if (!seen) { set_error("no host memory for the check of %d pages", cache->n_pages); return LUVC_ERR_WORKSPACE; }
+    // a page is written once and never read: few pairs are compared with each other, for more there is a mark per page
     int bad = -1;
-    for (int i = 0; i < n; ++i) seen[src[i]] = 1;
-    for (int i = 0; i < n && bad < 0; ++i) {
-        if (seen[dst[i]]) bad = i;
-        seen[dst[i]] = 2;
+    if (n <= 16) {
+        for (int i = 0; i < n && bad < 0; ++i)
+            for (int j = 0; j < n; ++j)
+                if (dst[i] == src[j] || (j < i && dst[i] == dst[j])) bad = i;
+    } else {
+        unsigned char* seen = (unsigned char*)calloc((size_t)cache->n_pages, 1);
+        if (!seen) { set_error("no host memory for the check of %d pages", cache->n_pages); return LUVC_ERR_WORKSPACE; }
+        for (int i = 0; i < n; ++i) seen[src[i]] = 1;
+        for (int i = 0; i < n && bad < 0; ++i) {
+            if (seen[dst[i]]) bad = i;
+            seen[dst[i]] = 2;
+        }
+        free(seen);
     }
-    free(seen);
     if (bad >= 0) { set_error("pair %d: page %d is written to and in use by another pair", bad, dst[bad]); return LUVC_ERR_INVALID_ARG; }
     return kv_copy_run(*cache, src, 1, dst, 1, n, cache->page_tokens, (hipStream_t)hip_stream);
 }

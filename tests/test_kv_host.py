@@ -192,6 +192,30 @@ def test_take_and_release_against_a_model(L):
         assert refs.tolist() == model
 
 
+@pytest.mark.parametrize("n_pages", [1, 15, 16, 17, 33, 1000, 4096])
+def test_take_finds_the_last_free_pages(L, n_pages):
+    rng = random.Random(n_pages)
+    free = sorted(rng.sample(range(n_pages), min(n_pages, 5)) + ([n_pages - 1] if n_pages > 5 else []))
+    free = sorted(set(free))
+    refs = torch.ones(n_pages, dtype=torch.int32)
+    refs[free] = 0
+    with pytest.raises(lv.LuvcError):
+        lv.luvc_kv_take(refs, len(free) + 1)
+    assert lv.luvc_kv_take(refs, len(free)).tolist() == free and bool((refs == 1).all())
+
+
+@pytest.mark.parametrize("pairs", [1, 2, 16, 17, 200])
+def test_copy_refusals_at_any_place(L, pairs):
+    c = cache(n_pages=500, layer_stride=1 << 30)
+    for bad in range(0, pairs, max(1, pairs // 7)):
+        src, dst = [i // 2 for i in range(pairs)], [200 + i for i in range(pairs)]
+        for page in {src[-1], src[bad], dst[bad - 1] if pairs > 1 else src[0]}:
+            broken = list(dst)
+            broken[bad] = page
+            assert L.luvc_kv_copy_pages(ctypes.byref(c), i32(*src), i32(*broken), pairs, None) == lv.LUVC_ERR_INVALID_ARG, (pairs, bad, page)
+            assert "written to" in lv.last_error()
+
+
 def test_release_refusals_leave_the_counts(L):
     refs = torch.tensor([2, 1, 0], dtype=torch.int32)
     for bad in ([0, 0, 0], [1, 2], [0, -1], [0, 3], [1, 1]):
