@@ -99,7 +99,7 @@ struct KvWork {
 // Sequences of 1 to 32768 tokens, 16 of them, 4 heads of 128, bf16: 107 us without the third cut (544 runs for 512 places), 93 with it;
 // 16 of 4096 in fp32, which fit two to a unit: 54 cut for three, 47 for two; five to a unit are no better, and 128 of 1024 take 50 for 43.
 // Against runs by the bound on the lengths it is one more trip to memory, 0.7 us, and
-//   64 sequences of 1 to 8200 tokens, 8 heads: 68.5 us by the bound (3500 of 4600 runs empty and others waiting for them), 57
+//   64 sequences of 1 to 8200 tokens, 8 heads: 68.5 us by the bound (3500 of 4600 runs empty and others waiting for them), 55.5
 //   300 of 1 to 2000 with a bound of 32768: 313, 202.  One of 4000 with a bound of 131072: 14.6, 9.4.  One of 32768 and no other: 28.1, 26.6
 //   1000 of 100 with a bound of 4096, what it serves worst: 125, 130
 // kFinest * kUnits / n_parts + n runs at most, n <= 1024 sequences.  Every 64th sequence belongs to a lane.
