@@ -93,19 +93,22 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
     return kv_write_run(*cache, layer, k, k_stride, v, v_stride, sizes, tokens, seq, pos, table, n_seqs, max_pages, (hipStream_t)hip_stream);
 }
 
-static bool attend_sizes_ok(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens)
+static bool attend_sizes_ok(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens, luvc_status* rc)
 {
+    *rc = LUVC_ERR_INVALID_ARG;
     if (n_seqs < 1 || n_q_heads < 1 || max_tokens < 1) { set_error("n_seqs, n_q_heads and max_tokens must be positive (got %d, %d, %d)", n_seqs, n_q_heads, max_tokens); return false; }
     if (n_q_heads % cache->n_heads) { set_error("n_q_heads=%d is no multiple of the cache's %d heads", n_q_heads, cache->n_heads); return false; }
+    *rc = LUVC_ERR_UNSUPPORTED;
     if (max_tokens >= (1 << 30)) { set_error("max_tokens must stay below 2^30"); return false; }
     if ((int64_t)n_seqs * n_q_heads >= ((int64_t)1 << 22)) { set_error("n_seqs * n_q_heads must stay below 2^22"); return false; }
+    *rc = LUVC_OK;
     return true;
 }
 
 size_t luvc_kv_attend_workspace_bytes(const luvc_kv_cache* cache, int n_seqs, int n_q_heads, int max_tokens)
 {
     luvc_status rc;
-    if (!cache_shape_ok(cache, &rc) || !attend_sizes_ok(cache, n_seqs, n_q_heads, max_tokens)) return 0;
+    if (!cache_shape_ok(cache, &rc) || !attend_sizes_ok(cache, n_seqs, n_q_heads, max_tokens, &rc)) return 0;
     return kv_attend_workspace(n_seqs, n_q_heads, cache->n_heads, cache->D, cache->dtype, max_tokens);
 }
 
@@ -116,7 +119,7 @@ luvc_status luvc_kv_attend(const luvc_kv_cache* cache, int layer, const void* q,
     luvc_status rc;
     if (!layer_ok(cache, layer, &rc)) return rc;
     if (!q || !table || !lengths || !out) { set_error("q, table, lengths and out must not be NULL"); return LUVC_ERR_INVALID_ARG; }
-    if (!attend_sizes_ok(cache, n_seqs, n_q_heads, max_tokens)) return LUVC_ERR_INVALID_ARG;
+    if (!attend_sizes_ok(cache, n_seqs, n_q_heads, max_tokens, &rc)) return rc;
     if (max_pages < 1) { set_error("max_pages must be positive"); return LUVC_ERR_INVALID_ARG; }
     const int64_t row = (int64_t)n_q_heads * cache->D;
     if (q_stride < row || out_stride < row) { set_error("sequence strides must be at least n_q_heads * D = %lld", (long long)row); return LUVC_ERR_INVALID_ARG; }

@@ -80,9 +80,11 @@ def test_attend_refusals_and_workspace(L):
                                       kw.get("out", FAKE), kw.get("os", 512), kw.get("ws"), kw.get("wsb", 0), None)
     for bad in (dict(layer=2), dict(q=None), dict(table=None), dict(lengths=None), dict(out=None), dict(hq=0), dict(hq=6), dict(S=0), dict(mp=0), dict(most=0),
                 dict(qs=511), dict(os=511), dict(q=ctypes.c_void_p(0x1001)), dict(out=ctypes.c_void_p(0x1001)), dict(scale=ctypes.byref(nan)),
-                dict(c=cache(sizes=None), enhance=1), dict(S=1 << 21)):
+                dict(c=cache(sizes=None), enhance=1)):
         assert a(**bad) == lv.LUVC_ERR_INVALID_ARG, bad
         assert lv.last_error()
+    for beyond in (dict(S=1 << 21), dict(S=1 << 19), dict(most=1 << 30)):
+        assert a(**beyond) == lv.LUVC_ERR_UNSUPPORTED, beyond
     need = L.luvc_kv_attend_workspace_bytes(ctypes.byref(c), 2, 8, 64)
     assert need >= 256 and need % 256 == 0
     assert a(scale=ctypes.byref(one)) == lv.LUVC_ERR_WORKSPACE
