@@ -380,8 +380,8 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
  *               captured call may have a bound far above them; beyond, and for the workspace, by the bound
  *   scale       host, or NULL: 1 / sqrt(D); twice its value must be finite in fp32
  *   enhance     0: the plain values v_j; else the term log s_j as well (needs a cache with sizes)
- * Logits, softmax and sums are fp32; with bf16 the weights a_j enter the product with the values in two bf16 terms (16 bits)
- * and the output is rounded once.  The parts of a long sequence are joined in a fixed order: same input, same bits.
+ * Logits, softmax, weights and sums are fp32 and the output is rounded once.  The parts of a long sequence are joined in a
+ * fixed order: same input, same bits.
  * Keys and values of the tokens that take part are finite; what the others' places hold does not matter.
  * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype), which is enough for fewer
  * sequences and a smaller max_tokens as well; any contents, one per call in flight, also for calls in captured graphs.
