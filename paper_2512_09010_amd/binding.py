@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
+from contextlib import nullcontext
 from itertools import chain
 from typing import List, Optional, Sequence, Tuple
 
@@ -142,6 +143,9 @@ def lib() -> ctypes.CDLL:
     return L
 
 
+_as_it_is = nullcontext()
+
+
 class _Native:
     """What a call needs at hand: torch, the caller, the addresses of the entry points."""
 
@@ -167,6 +171,22 @@ class _Native:
 
     def stream(self, stream) -> int:
         return self.raw_stream(self.device()) if stream is None else int(stream.cuda_stream)
+
+    def elsewhere(self, stream) -> bool:
+        return stream is not None and int(stream.cuda_stream) != self.raw_stream(self.device())
+
+    def allocating(self, stream):
+        """Where a call on `stream` allocates: among that stream's own blocks.  One of the current stream's is free when the current stream has
+        come so far; another stream would have it while earlier work, or a call without a workspace on the current stream, still uses it."""
+        return self.torch.cuda.stream(stream) if self.elsewhere(stream) else _as_it_is
+
+    def hand_over(self, stream, *tensors):
+        """Outputs allocated for a call on `stream` will be used on the current one: freed, they are not reused before that has come so far too."""
+        if self.elsewhere(stream):
+            here = self.torch.cuda.current_stream()
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(here)
 
 
 _native_state = None
@@ -656,7 +676,7 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
                    enhance: bool = False, workspace=None, stream=None, out=None):
     """q [n_seqs, n_q_heads, D] (dense heads, sequences evenly strided): one new token per sequence attends to the lengths [n_seqs] int32
     tokens in the pages of table [n_seqs, max_pages].  max_tokens: no sequence is longer (None: what the table holds).
-    Returns out [n_seqs, n_q_heads, D]."""
+    Returns out [n_seqs, n_q_heads, D].  With a stream, what is allocated here is that stream's; waiting for it is the caller's part."""
     nat = _native()
     shape, i32, dtype = q.shape, nat.i32, cache.dtype
     S, Hq, D = shape
@@ -668,11 +688,12 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
         max_tokens = min(max(width * cache.page_tokens, 1), (1 << 30) - 1)
     if workspace is None:
         need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
-        if stream is not None:                         # it is freed on return, before another stream may have come to the call
-            workspace.record_stream(stream)
+        with nat.allocating(stream):
+            workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
     if out is None:
-        out = nat.torch.empty(shape, dtype=dtype, device=q.device)
+        with nat.allocating(stream):
+            out = nat.torch.empty(shape, dtype=dtype, device=q.device)
+        nat.hand_over(stream, out)
     assert out.shape == shape and out.dtype is dtype
     _here(nat, cache, q, table, lengths, workspace, out)
     sc = None if scale is None else ctypes.c_double(scale)
