@@ -180,13 +180,21 @@ class _Native:
         come so far; another stream would have it while earlier work, or a call without a workspace on the current stream, still uses it."""
         return self.torch.cuda.stream(stream) if self.elsewhere(stream) else _as_it_is
 
-    def hand_over(self, stream, *tensors):
-        """Outputs allocated for a call on `stream` will be used on the current one: freed, they are not reused before that has come so far too."""
-        if self.elsewhere(stream):
-            here = self.torch.cuda.current_stream()
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(here)
+    def scratch(self, stream, need, device):
+        with self.allocating(stream):
+            return self.torch.empty(max(need, 256), dtype=self.torch.uint8, device=device)
+
+    def outputs(self, stream, make):
+        """make() is a tensor or a dict of them.  They will be used on the current stream: freed, they are not reused before that has come so far too."""
+        if not self.elsewhere(stream):
+            return make()
+        with self.allocating(stream):
+            out = make()
+        here = self.torch.cuda.current_stream()
+        for t in out.values() if isinstance(out, dict) else (out,):
+            if t is not None:
+                t.record_stream(here)
+        return out
 
 
 _native_state = None
@@ -311,9 +319,9 @@ def luvc_oim_merge(x, passes, sizes=None, target_tokens: int = 0, want_maps: boo
     arr, addr, n = _schedule(passes)
     if workspace is None:
         need = lib().luvc_oim_workspace_bytes(B, H, W, D, code, arr, n)
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, need, x.device)
     if out is None:
-        out = _merge_outputs(nat.torch, x, *out_grid(H, W, passes), want_maps)
+        out = nat.outputs(stream, lambda: _merge_outputs(nat.torch, x, *out_grid(H, W, passes), want_maps))
     if sizes is not None:
         assert sizes.is_cuda and sizes.dtype == nat.i32 and sizes.is_contiguous() and sizes.numel() == B * H * W
         sizes = sizes.data_ptr()
@@ -337,9 +345,9 @@ def luvc_oim_merge_wide(x, passes, radius: int, sizes=None, target_tokens: int =
     arr, addr, n = _schedule(passes)
     if workspace is None:
         need = lib().luvc_oim_wide_workspace_bytes(B, H, W, D, code, arr, n, int(radius))
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, need, x.device)
     if out is None:
-        out = _merge_outputs(nat.torch, x, *out_grid(H, W, passes), want_maps)
+        out = nat.outputs(stream, lambda: _merge_outputs(nat.torch, x, *out_grid(H, W, passes), want_maps))
     if sizes is not None:
         assert sizes.is_cuda and sizes.dtype == nat.i32 and sizes.is_contiguous() and sizes.numel() == B * H * W
         sizes = sizes.data_ptr()
@@ -365,11 +373,12 @@ def luvc_oim_merge_keyed(x, metric, passes, radius: int = 1, sizes=None, target_
     arr, addr, n = _schedule(passes)
     if workspace is None:
         need = lib().luvc_oim_keyed_workspace_bytes(B, H, W, D, Dm, code, arr, n, int(radius))
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, need, x.device)
     if out is None:
         Ho, Wo = out_grid(H, W, passes)
-        out = _merge_outputs(nat.torch, x, Ho, Wo, want_maps)
-        out["metric"] = nat.torch.empty((B, max(Ho, 0), max(Wo, 0), Dm), dtype=x.dtype, device=x.device) if want_metric else None
+        out = nat.outputs(stream, lambda: dict(
+            _merge_outputs(nat.torch, x, Ho, Wo, want_maps),
+            metric=nat.torch.empty((B, max(Ho, 0), max(Wo, 0), Dm), dtype=x.dtype, device=x.device) if want_metric else None))
     if sizes is not None:
         assert sizes.is_cuda and sizes.dtype == nat.i32 and sizes.is_contiguous() and sizes.numel() == B * H * W
         sizes = sizes.data_ptr()
@@ -388,7 +397,7 @@ def luvc_value_enhance(v, sizes, stream=None, out=None):
     rows = sizes.numel()
     assert v.numel() == rows * D and v.is_contiguous()
     if out is None:
-        out = nat.torch.empty_like(v)
+        out = nat.outputs(stream, lambda: nat.torch.empty_like(v))
     _check(nat.call(nat.luvc_value_enhance, v.data_ptr(), sizes.data_ptr(), rows, D, D, _dtype_code(v), out.data_ptr(), D, nat.stream(stream)))
     return out
 
@@ -406,9 +415,9 @@ def luvc_spu_score(x, sigma: int, use_hamming: bool = True, workspace=None, stre
     code = _dtype_code(x)
     if workspace is None:
         need = lib().luvc_spu_workspace_bytes(B, N, D, code, int(sigma))
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, need, x.device)
     if out is None:
-        out = nat.torch.empty((B, N), dtype=nat.f32, device=x.device)
+        out = nat.outputs(stream, lambda: nat.torch.empty((B, N), dtype=nat.f32, device=x.device))
     _check(nat.call(nat.luvc_spu_score, x.data_ptr(), B, N, D, sn, code, int(sigma), int(bool(use_hamming)), out.data_ptr(),
                     workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
     return out
@@ -423,7 +432,7 @@ def luvc_spu_score_static(x, sigma: int, use_hamming: bool = True, stream=None, 
     assert x.is_cuda and x.dim() == 3 and x.stride(2) == 1 and x.stride(0) == x.shape[1] * x.stride(1)
     B, N, D = x.shape
     if out is None:
-        out = nat.torch.empty((B, N), dtype=nat.f32, device=x.device)
+        out = nat.outputs(stream, lambda: nat.torch.empty((B, N), dtype=nat.f32, device=x.device))
     _check(nat.call(nat.luvc_spu_score_static, x.data_ptr(), B, N, D, x.stride(1), _dtype_code(x), int(sigma), int(bool(use_hamming)),
                     out.data_ptr(), nat.stream(stream)))
     return out
@@ -439,8 +448,9 @@ def luvc_spu_prune(x, scores, n_keep: int, gather: bool = True, stream=None, out
         assert x.is_cuda and x.dim() == 3 and x.stride(2) == 1 and x.shape[:2] == scores.shape
         D, stride, code, xp = x.shape[2], x.stride(1), _dtype_code(x), x.data_ptr()
     if out is None:
-        out = dict(kept_idx=nat.torch.empty((B, max(n_keep, 0)), dtype=nat.i32, device=scores.device),
-                   x=nat.torch.empty((B, max(n_keep, 0), D), dtype=x.dtype, device=x.device) if (gather and x is not None) else None)
+        out = nat.outputs(stream, lambda: dict(
+            kept_idx=nat.torch.empty((B, max(n_keep, 0)), dtype=nat.i32, device=scores.device),
+            x=nat.torch.empty((B, max(n_keep, 0), D), dtype=x.dtype, device=x.device) if (gather and x is not None) else None))
     _check(nat.call(nat.luvc_spu_prune, xp, scores.data_ptr(), B, N, D, stride, code, int(n_keep), out["kept_idx"].data_ptr(),
                     _ptr(out.get("x")), None, 0, nat.stream(stream)))
     return out
@@ -470,12 +480,13 @@ def luvc_spu_stage(x, sigma: int, n_keep: int, use_hamming: bool = True, origin=
     k = max(int(n_keep), 0)
     if workspace is None:
         need = lib().luvc_spu_workspace_bytes(B, N, D, code, int(sigma)) if k else 0
-        workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, need, x.device)
     if out is None:
-        out = dict(scores=nat.torch.empty((B, N), dtype=nat.f32, device=x.device),
-                   kept_idx=nat.torch.empty((B, k), dtype=nat.i32, device=x.device),
-                   origin=nat.torch.empty((B, k), dtype=nat.i32, device=x.device),
-                   x=nat.torch.empty((B, k, D), dtype=x.dtype, device=x.device) if gather else None)
+        out = nat.outputs(stream, lambda: dict(
+            scores=nat.torch.empty((B, N), dtype=nat.f32, device=x.device),
+            kept_idx=nat.torch.empty((B, k), dtype=nat.i32, device=x.device),
+            origin=nat.torch.empty((B, k), dtype=nat.i32, device=x.device),
+            x=nat.torch.empty((B, k, D), dtype=x.dtype, device=x.device) if gather else None))
     _check(nat.call(nat.luvc_spu_stage, x.data_ptr(), B, N, D, sn, code, int(sigma), int(bool(use_hamming)), int(n_keep),
                     origin, out["scores"].data_ptr(), out["kept_idx"].data_ptr(), out["origin"].data_ptr(),
                     _ptr(out.get("x")), workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
@@ -536,18 +547,18 @@ def luvc_oim_merge_ragged(x, shapes, schedules, sizes=None, want_maps: bool = Tr
     assert T == plan.tokens_in
     To = plan.tokens_out
     if workspace is None:
-        workspace = torch.empty(max(plan.need, 256), dtype=torch.uint8, device=x.device)
+        workspace = nat.scratch(stream, plan.need, x.device)
     if sizes is not None:
         assert sizes.is_cuda and sizes.dtype == nat.i32 and sizes.is_contiguous() and sizes.numel() == T
         sizes = sizes.data_ptr()
-    xo = torch.empty((To, D), dtype=x.dtype, device=x.device)
-    so = torch.empty((To,), dtype=nat.i32, device=x.device)
-    merged = torch.empty((T,), dtype=nat.i32, device=x.device) if want_maps else None
-    kept = torch.empty((To,), dtype=nat.i32, device=x.device) if want_maps else None
+    i32 = dict(dtype=nat.i32, device=x.device)
+    out = nat.outputs(stream, lambda: dict(
+        x=torch.empty((To, D), dtype=x.dtype, device=x.device), sizes=torch.empty((To,), **i32),
+        merged_map=torch.empty((T,), **i32) if want_maps else None, kept_map=torch.empty((To,), **i32) if want_maps else None))
     H, W, passes, n_passes = plan.addr
-    _check(nat.call(nat.luvc_oim_merge_ragged, x.data_ptr(), sizes, plan.n, H, W, D, code, passes, n_passes, xo.data_ptr(), so.data_ptr(),
-                    _ptr(merged), _ptr(kept), workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
-    return dict(x=xo, sizes=so, merged_map=merged, kept_map=kept, out_shapes=list(plan.out_shapes))
+    _check(nat.call(nat.luvc_oim_merge_ragged, x.data_ptr(), sizes, plan.n, H, W, D, code, passes, n_passes, out["x"].data_ptr(), out["sizes"].data_ptr(),
+                    _ptr(out["merged_map"]), _ptr(out["kept_map"]), workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
+    return dict(out, out_shapes=list(plan.out_shapes))
 
 
 class _RaggedStage:
@@ -592,17 +603,19 @@ def luvc_spu_stage_ragged(x, lengths, sigmas, keeps=None, use_hamming: bool = Tr
         assert origin.is_cuda and origin.dtype == nat.i32 and origin.is_contiguous() and origin.numel() == T
         origin = origin.data_ptr()
     if workspace is None:
-        workspace = torch.empty(max(plan.need, 256), dtype=torch.uint8, device=x.device)
-    scores = torch.empty((T,), dtype=nat.f32, device=x.device)
-    kept_idx, kept_origin = torch.empty((K,), dtype=nat.i32, device=x.device), torch.empty((K,), dtype=nat.i32, device=x.device)
-    xo = torch.empty((K, D), dtype=x.dtype, device=x.device) if (gather and keeps is not None) else None
+        workspace = nat.scratch(stream, plan.need, x.device)
+    out = nat.outputs(stream, lambda: dict(
+        scores=torch.empty((T,), dtype=nat.f32, device=x.device),
+        kept_idx=torch.empty((K,), dtype=nat.i32, device=x.device), origin=torch.empty((K,), dtype=nat.i32, device=x.device),
+        x=torch.empty((K, D), dtype=x.dtype, device=x.device) if (gather and keeps is not None) else None))
+    scores, kept_idx, kept_origin, xo = out["scores"], out["kept_idx"], out["origin"], out["x"]
     # a tensor without elements has no address: hand the library one it will not touch
     ki = kept_idx.data_ptr() if K else scores.data_ptr()
     og = kept_origin.data_ptr() if K else scores.data_ptr()
     N, sigma, keep = plan.addr
     _check(nat.call(nat.luvc_spu_stage_ragged, x.data_ptr(), plan.n, N, D, x.stride(0), code, sigma, int(bool(use_hamming)), keep,
                     origin, scores.data_ptr(), ki, og, _ptr(xo) if K else None, workspace.data_ptr(), workspace.numel(), nat.stream(stream)))
-    return dict(scores=scores, kept_idx=kept_idx, origin=kept_origin, x=xo)
+    return out
 
 
 class KvCache:
@@ -688,12 +701,9 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
         max_tokens = min(max(width * cache.page_tokens, 1), (1 << 30) - 1)
     if workspace is None:
         need = luvc_kv_attend_workspace_bytes(cache, S, Hq, max_tokens)
-        with nat.allocating(stream):
-            workspace = nat.torch.empty(max(need, 256), dtype=nat.torch.uint8, device=q.device)
+        workspace = nat.scratch(stream, need, q.device)
     if out is None:
-        with nat.allocating(stream):
-            out = nat.torch.empty(shape, dtype=dtype, device=q.device)
-        nat.hand_over(stream, out)
+        out = nat.outputs(stream, lambda: nat.torch.empty(shape, dtype=dtype, device=q.device))
     assert out.shape == shape and out.dtype is dtype
     _here(nat, cache, q, table, lengths, workspace, out)
     sc = None if scale is None else ctypes.c_double(scale)
