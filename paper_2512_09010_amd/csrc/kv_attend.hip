@@ -258,9 +258,10 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         splits = len > chunk ? (len + chunk - 1) / chunk : 1;
         if (split >= splits) return;
     }
-    // Arrival words: the sequence's, then those of its groups of runs.  A word is the process's tag and a count; one without the tag is
-    // taken over by whoever may come to it first (thread 0: the word of this run; thread 1 of a group's first run: the sequence's, to which
-    // the group comes when all of it has arrived), and whoever completes a count leaves the tag and zero behind.
+    // Arrival words: the sequence's, then those of its groups of runs.  A word is the launch's tag and a count; one without the tag, whatever an
+    // earlier launch or anything else left there, is taken over by whoever may come to it first (thread 0: the word of this run; thread 1 of a
+    // group's first run: the sequence's, to which the group comes when all of it has arrived), and whoever completes a count leaves zero
+    // behind, so that a captured launch starts over the same way.
     const bool grouped = splits > kDirect;
     tile_tag_t* const words = wk.words + (((int64_t)s * wk.n_heads + h) * wk.tiles + qt) * wk.words_each;
     tile_tag_t* word = words + (grouped ? 1 + split / kFan : 0);
@@ -567,7 +568,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         if (tid == 0) {
             const tile_tag_t old = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             last_flag = (int)(old & 0xffffu) == runs - 1;
-            if (last_flag) tag_store(word, wk.tag << 16);
+            if (last_flag) tag_store(word, 0ull);
         }
         __syncthreads();
         if (!last_flag) return;
@@ -756,7 +757,7 @@ size_t kv_attend_workspace(int n_seqs, int n_q_heads, int n_heads, int D, luvc_d
 luvc_status kv_attend_run(const luvc_kv_cache& c, int layer, const KvAttend& a, void* ws, hipStream_t st)
 {
     const AttendPlan p = attend_plan(a.n_seqs, a.n_q_heads, c.n_heads, c.D, c.dtype, a.max_tokens);
-    static const tile_tag_t tag = spu_next_tag();
+    const tile_tag_t tag = spu_next_tag();
     const double log2e = 1.4426950408889634074, full = a.scale == 0.0 ? 1.0 : std::fabs(a.scale) * log2e;
     const float scale = (float)full, rest = (float)(full - scale);
     const KvWork wk{c.sizes, c.n_pages, c.n_heads, kv_log2_page(c), c.D, a.n_q_heads / c.n_heads, p.chunk, p.tiles, p.cols, p.parts_row, p.words_each, p.lds_words, p.planned,
