@@ -222,9 +222,10 @@ luvc_status luvc_kv_fork(const luvc_kv_cache* cache, int32_t* refs, const int32_
     if (!cache_ok(cache, &rc)) return rc;
     if (length < 1 || n_children < 1) { set_error("length and n_children must be positive"); return LUVC_ERR_INVALID_ARG; }
     if (!refs || !pages || !child_pages) { set_error("refs, pages and child_pages must not be NULL"); return LUVC_ERR_INVALID_ARG; }
-    const int64_t P = cache->page_tokens, full = length / P, all = (length + P - 1) / P;
+    const int64_t P = cache->page_tokens;
+    if (length > cache->n_pages * P) { set_error("%lld tokens do not fit %d pages", (long long)length, cache->n_pages); return LUVC_ERR_INVALID_ARG; }
+    const int64_t full = length / P, all = (length + P - 1) / P;
     const int rows = (int)(length % P);
-    if (all > cache->n_pages) { set_error("%lld tokens do not fit %d pages", (long long)length, cache->n_pages); return LUVC_ERR_INVALID_ARG; }
     for (int64_t j = 0; j < all; ++j) {
         if (pages[j] < 0 || pages[j] >= cache->n_pages || refs[pages[j]] < 1) {
             set_error("page %d at %lld of the sequence is not in use", pages[j], (long long)j);
