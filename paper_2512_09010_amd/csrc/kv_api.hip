@@ -226,22 +226,30 @@ luvc_status luvc_kv_fork(const luvc_kv_cache* cache, int32_t* refs, const int32_
     if (length > cache->n_pages * P) { set_error("%lld tokens do not fit %d pages", (long long)length, cache->n_pages); return LUVC_ERR_INVALID_ARG; }
     const int64_t full = length / P, all = (length + P - 1) / P;
     const int rows = (int)(length % P);
-    for (int64_t j = 0; j < all; ++j) {
+    for (int64_t j = 0; j < all; ++j)
         if (pages[j] < 0 || pages[j] >= cache->n_pages || refs[pages[j]] < 1) {
             set_error("page %d at %lld of the sequence is not in use", pages[j], (long long)j);
             return LUVC_ERR_INVALID_ARG;
         }
-        if (refs[pages[j]] > INT32_MAX - n_children) { set_error("page %d would count too many sequences", pages[j]); return LUVC_ERR_INVALID_ARG; }
+    // counted one by one: a sequence may hold a page at several places
+    auto uncount = [&](int64_t n) { while (n-- > 0) refs[pages[n]] -= n_children; };
+    for (int64_t j = 0; j < full; ++j) {
+        if (refs[pages[j]] > INT32_MAX - n_children) {
+            set_error("page %d would count too many sequences", pages[j]);
+            uncount(j);
+            return LUVC_ERR_INVALID_ARG;
+        }
+        refs[pages[j]] += n_children;
     }
     if (rows) {
-        if (!take(refs, cache->n_pages, n_children, child_pages + full, all)) return LUVC_ERR_WORKSPACE;
+        if (!take(refs, cache->n_pages, n_children, child_pages + full, all)) { uncount(full); return LUVC_ERR_WORKSPACE; }
         rc = kv_copy_run(*cache, pages + full, 0, child_pages + full, (int)all, n_children, rows, (hipStream_t)hip_stream);
         if (rc != LUVC_OK) {
             for (int i = 0; i < n_children; ++i) refs[child_pages[i * all + full]] = 0;
+            uncount(full);
             return rc;
         }
     }
-    for (int64_t j = 0; j < full; ++j) refs[pages[j]] += n_children;
     for (int i = 0; i < n_children; ++i)
         for (int64_t j = 0; j < full; ++j) child_pages[i * all + j] = pages[j];
     return LUVC_OK;
