@@ -382,7 +382,9 @@ luvc_status luvc_kv_write(const luvc_kv_cache* cache, int layer, const void* k, 
  *   enhance     0: the plain values v_j; else the term log s_j as well (needs a cache with sizes)
  * Logits, softmax, weights and sums are fp32 and the output is rounded once.  The parts of a long sequence are joined in a
  * fixed order: same input, same bits.
- * Keys and values of the tokens that take part are finite; what the others' places hold does not matter.
+ * Queries, and keys and values of the tokens that take part, are finite, and so are in fp32 <q[s,h], k_j> before its scale and 256 times
+ * the sum of |v_j| over a sequence (sums run over weights of up to 256, divided at the end); what the others' places hold
+ * does not matter.
  * Workspace: luvc_kv_attend_workspace_bytes (of the cache's fields it reads n_heads, D and dtype), which is enough for fewer
  * sequences and a smaller max_tokens as well; any contents, one per call in flight, also for calls in captured graphs.
  * Limits: n_seqs * n_q_heads < 2^22, max_tokens < 2^30.

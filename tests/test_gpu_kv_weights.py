@@ -50,3 +50,21 @@ def test_weights_of_bf16_caches_keep_the_bits_of_fp32(D, spare):
     tol = 2.0 ** -8 * np.abs(want) + 26 * 2.0 ** -24 * (p / total)[:, :, None]
     off = np.abs(out - want) - tol
     assert (off <= 0).all(), (int((off > 0).sum()), off.size, float((np.abs(out - want) / (p / total)[:, :, None]).max() * 2 ** 24))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("up", [100, -60])
+def test_magnitudes_of_values_and_logits(dtype, up):
+    """Values times a power of two give the output times that power, bit for bit, and so do keys for queries divided by it: nothing on the way
+    leaves the range of fp32 (256 times a sum of 900 values of 2^100 is 2^118)."""
+    gen = torch.Generator(device="cuda").manual_seed(90)
+    S, H, P, D, width = 2, 2, 16, 64, 57
+    k, v = (torch.randn((1, S * width, H, P, D), generator=gen, device="cuda").clamp(-4, 4).to(dtype) for _ in range(2))
+    q = torch.randn((S, 4, D), generator=gen, device="cuda").to(dtype)
+    table = torch.arange(S * width, dtype=torch.int32, device="cuda").view(S, width)
+    n = torch.tensor([900, 33], dtype=torch.int32, device="cuda")
+    f = 2.0 ** up
+    want = lv.luvc_kv_attend(lv.KvCache(k, v), 0, q, table, n)
+    assert torch.equal(lv.luvc_kv_attend(lv.KvCache(k, v * f), 0, q, table, n), want * f)
+    g = 2.0 ** (up // 2)
+    assert torch.equal(lv.luvc_kv_attend(lv.KvCache(k * g, v), 0, q / g, table, n), want)
