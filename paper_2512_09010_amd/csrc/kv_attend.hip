@@ -16,9 +16,9 @@
 //               a channel side by side
 // The next step's keys are asked for when this one's are in LDS, its values when this one's are used up; four wavefronts of a step each in
 // flight, and two or three workgroups to a unit, keep memory busy (eight wavefronts to a workgroup were no faster, and their join slower).
-// With bf16 the second product takes a weight in three bf16 terms, 8 bits each, which together are its fp32 value: with one the weights would be
-// rounded as coarsely as the output, with two by up to 2^-17, and the matrix cores have the time (64 x 4096: 161 us with two, 161 with three; the
-// queries are read from LDS at every step instead of kept in registers, which a third term would push to scratch memory: 170).
+// With bf16 the second product takes a weight in three bf16 terms, which together are its fp32 value: with one the weights would be rounded as
+// coarsely as the output, with two by up to 2^-17, and the matrix cores have the time (64 x 4096: 161 us with two, 161 with three; where steps
+// do without memory, nine tokens in ten dead, 55 and 58).
 // The maximum is raised (and what has been summed scaled down) only when a logit exceeds it by more than 8 in powers of two: p stays
 // below 256, and most steps do without an exchange between lanes.
 // Tokens behind the end, without a page or of size below 1 get z = -inf and zeros for values, whatever their rows hold.
@@ -341,6 +341,15 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
         ask_values(~0u);
     }
     __syncthreads();                                          // the queries are in LDS
+    // Read from there at every step; kept where the sizes' variant has the registers (8 x 1100 tokens: 9.1 us for 9.3; kept in both, the other
+    // one's 128 channels go to scratch memory, 64 x 4096: 170 us for 161)
+    constexpr bool KEEP = SIZED;
+    auto query = [&](int n) { return *(const kv_u32x4*)(queries + (c * (PIECES + 1) + 4 * n + g) * 16); };
+    kv_u32x4 kept[KEEP ? NK : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int n = 0; n < NK; ++n) kept[n] = query(n);
+    }
     kv_f32x4 o[NV * VL] = {};
     float m = kLowest, l = 0.f, ls = 0.f;
     uint32_t live = live_at(t0, pages0, size);
@@ -363,7 +372,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
                 const kv_u32x4 kf = *(const kv_u32x4*)(keys + (i * 16 + c) * PIECES * 16 + (((4 * n + g) ^ (c & SWZ)) * 16));
-                const kv_u32x4 qf = *(const kv_u32x4*)(queries + (c * (PIECES + 1) + 4 * n + g) * 16);
+                const kv_u32x4 qf = KEEP ? kept[KEEP ? n : 0] : query(n);
                 if constexpr (BF) {
                     z[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_bf16x8, kf), __builtin_bit_cast(kv_bf16x8, qf), z[0], 0, 0, 0);
                 } else {
@@ -427,17 +436,16 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                     for (int w = 0; w < VW; ++w) vf[j][n][w] = on(j) ? vf[j][n][w] : 0u;
         }
         if constexpr (BF) {
-            kv_u32x4 term[3];                                 // of the weights, two tokens to a word: the upper half of what is left
+            kv_bf16x8 term[3];
 #pragma unroll
-            for (int i = 0; i < 3; ++i)
+            for (int j = 0; j < 8; ++j) {
+                float rest = p[j];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t a0 = __float_as_uint(p[2 * j]), a1 = __float_as_uint(p[2 * j + 1]);
-                    term[i][j] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
-                    if (i == 2) continue;
-                    p[2 * j] -= __uint_as_float(a0 & 0xffff0000u);
-                    p[2 * j + 1] -= __uint_as_float(a1 & 0xffff0000u);
+                for (int i = 0; i < 3; ++i) {
+                    term[i][j] = (__bf16)rest;
+                    rest -= (float)term[i][j];
                 }
+            }
 #pragma unroll
             for (int n = 0; n < NV; ++n)
 #pragma unroll
@@ -447,7 +455,7 @@ kv_attend(const T* __restrict__ kpool, const T* __restrict__ vpool, KvWork wk, K
                     for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(vf[2 * j + 1][n][e / 2], vf[2 * j][n][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
                     kv_f32x4& acc = o[n * VL + e];
 #pragma unroll
-                    for (int i = 0; i < 3; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_bf16x8, w), __builtin_bit_cast(kv_bf16x8, term[i]), acc, 0, 0, 0);
+                    for (int i = 0; i < 3; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_bf16x8, w), term[i], acc, 0, 0, 0);
                 }
         } else {
 #pragma unroll
