@@ -264,6 +264,14 @@ def _dtype_code(t) -> int:
     return code
 
 
+def _int32(value) -> int:
+    """An int of the library.  Of a longer one the call would see the lower 32 bits."""
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise LuvcError(LUVC_ERR_INVALID_ARG, f"{value} does not fit 32 bits")
+    return value
+
+
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -631,7 +639,7 @@ class KvCache:
         self.k, self.v, self.sizes = k, v, sizes
         L, n_pages, n_heads, P, D = k.shape
         stride = k.stride(0) if L > 1 else n_pages * n_heads * P * D
-        self.struct = LuvcKvCache(k.data_ptr(), v.data_ptr(), _ptr(sizes), stride, L, n_pages, n_heads, P, D, _dtype_code(k))
+        self.struct = LuvcKvCache(k.data_ptr(), v.data_ptr(), _ptr(sizes), stride, *map(_int32, k.shape), _dtype_code(k))
         self.addr = ctypes.addressof(self.struct)
         self.n_layers, self.n_pages, self.n_heads, self.page_tokens, self.D = L, n_pages, n_heads, P, D
         self.dtype, self.device = k.dtype, k.device
@@ -677,12 +685,12 @@ def luvc_kv_write(cache: KvCache, layer: int, k, v, pos, table, seq=None, sizes=
     assert pos.dtype is i32 and pos.is_contiguous() and pos.numel() == T
     assert seq is None or (seq.dtype is i32 and seq.is_contiguous() and seq.numel() == T)
     assert sizes is None or (sizes.dtype is i32 and sizes.is_contiguous() and sizes.numel() == T)
-    _check(nat.call(nat.luvc_kv_write, cache.addr, int(layer), k.data_ptr(), _rows(k, T, H, D), v.data_ptr(), _rows(v, T, H, D), _ptr(sizes), T, _ptr(seq),
+    _check(nat.call(nat.luvc_kv_write, cache.addr, _int32(layer), k.data_ptr(), _rows(k, T, H, D), v.data_ptr(), _rows(v, T, H, D), _ptr(sizes), T, _ptr(seq),
                     pos.data_ptr(), table.data_ptr(), n_seqs, width, nat.stream(stream)))
 
 
 def luvc_kv_attend_workspace_bytes(cache: KvCache, n_seqs: int, n_q_heads: int, max_tokens: int) -> int:
-    return lib().luvc_kv_attend_workspace_bytes(ctypes.byref(cache.struct), int(n_seqs), int(n_q_heads), int(max_tokens))
+    return lib().luvc_kv_attend_workspace_bytes(ctypes.byref(cache.struct), _int32(n_seqs), _int32(n_q_heads), _int32(max_tokens))
 
 
 def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Optional[int] = None, scale: Optional[float] = None,
@@ -707,8 +715,8 @@ def luvc_kv_attend(cache: KvCache, layer: int, q, table, lengths, max_tokens: Op
     assert out.shape == shape and out.dtype is dtype
     _here(nat, cache, q, table, lengths, workspace, out)
     sc = None if scale is None else ctypes.c_double(scale)
-    _check(nat.call(nat.luvc_kv_attend, cache.addr, int(layer), q.data_ptr(), _rows(q, S, Hq, D), Hq, S, table.data_ptr(), width, lengths.data_ptr(),
-                    int(max_tokens), None if sc is None else ctypes.addressof(sc), int(bool(enhance)), out.data_ptr(), _rows(out, S, Hq, D),
+    _check(nat.call(nat.luvc_kv_attend, cache.addr, _int32(layer), q.data_ptr(), _rows(q, S, Hq, D), Hq, S, table.data_ptr(), width, lengths.data_ptr(),
+                    _int32(max_tokens), None if sc is None else ctypes.addressof(sc), int(bool(enhance)), out.data_ptr(), _rows(out, S, Hq, D),
                     workspace.data_ptr(), workspace.nbytes, nat.stream(stream)))
     return out
 
@@ -747,22 +755,22 @@ def _refs(nat, refs):
 
 def luvc_kv_take(refs, n: int):
     """The n lowest pages that refs (CPU int32 [n_pages], changed in place) counts 0; they count 1 then.  Returns them, CPU int32 [n]."""
-    nat = _native()
-    pages = nat.torch.empty((max(int(n), 0),), dtype=nat.i32)
-    _check(nat.call(nat.luvc_kv_take, _refs(nat, refs), refs.numel(), int(n), pages.data_ptr() if n > 0 else None))
+    nat, n = _native(), _int32(n)
+    pages = nat.torch.empty((max(n, 0),), dtype=nat.i32)
+    _check(nat.call(nat.luvc_kv_take, _refs(nat, refs), refs.numel(), n, pages.data_ptr() if n > 0 else None))
     return pages
 
 
 def luvc_kv_fork(cache: KvCache, refs, pages, length: int, n_children: int, stream=None):
     """n_children sequences that go on from the `length` tokens in `pages` (host integers).  Returns their pages, CPU int32
     [n_children, ceil(length / page_tokens)]."""
-    nat = _native()
+    nat, n_children = _native(), _int32(n_children)
     _here(nat, cache)
     a, at, n = _host_ints(pages)
     used = -(-int(length) // cache.page_tokens)
     assert n >= used and refs.numel() == cache.n_pages
-    children = nat.torch.empty((max(int(n_children), 0), max(used, 0)), dtype=nat.i32)
-    _check(nat.call(nat.luvc_kv_fork, cache.addr, _refs(nat, refs), at, int(length), int(n_children), children.data_ptr(), nat.stream(stream)))
+    children = nat.torch.empty((max(n_children, 0), max(used, 0)), dtype=nat.i32)
+    _check(nat.call(nat.luvc_kv_fork, cache.addr, _refs(nat, refs), at, int(length), n_children, children.data_ptr(), nat.stream(stream)))
     return children
 
 

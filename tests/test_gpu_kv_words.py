@@ -54,3 +54,21 @@ def test_words_between_the_replays_of_a_graph(lengths, H, each):
         assert torch.equal(run(torch.empty_like(q)), want)
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """Layers, bounds and counts that would pass by their lower 32 bits."""
+    pool = Pool(72, [40, 20], 2, 64, "bf16", 16)
+    c, q, n, wide = pool.cache, pool.tensor(2, 4, 64), pool.tensor(2, 2, 64), 2 ** 32
+    refs = torch.ones(pool.n_pages, dtype=torch.int32)
+    refs[-4:] = 0
+    before = pool.kt.view(torch.int16).clone(), refs.clone()
+    for bad in (lambda: lv.luvc_kv_attend(c, wide, q, pool.tt, pool.lt), lambda: lv.luvc_kv_attend(c, 0, q, pool.tt, pool.lt, max_tokens=wide + 5),
+                lambda: lv.luvc_kv_attend(c, 0, q, pool.tt, pool.lt, max_tokens=wide + 5, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")),
+                lambda: lv.luvc_kv_attend_workspace_bytes(c, wide + 2, 4, 64), lambda: lv.luvc_kv_write(c, wide, n, n, pool.lt - 1, pool.tt),
+                lambda: lv.luvc_kv_fork(c, refs, [0], 5, wide + 1)):
+        with pytest.raises(lv.LuvcError) as e:
+            bad()
+        assert e.value.status == lv.LUVC_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(pool.kt.view(torch.int16), before[0]) and torch.equal(refs, before[1])

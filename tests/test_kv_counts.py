@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2512_09010_amd import binding as lv
 from test_kv_host import L, cache, i32  # noqa: F401  (L is a fixture)
@@ -36,3 +37,12 @@ def test_fork_without_a_free_page_takes_back_what_it_counted(L):  # noqa: F811
     refs = i32(*start)
     assert L.luvc_kv_fork(ctypes.byref(cache()), refs, i32(0, 1, 0, 2), 16 * 3 + 1, 1, i32(*[0] * 4), None) == lv.LUVC_ERR_WORKSPACE
     assert list(refs) == start
+
+
+def test_counts_beyond_32_bits():
+    """The library would see their lower 32 bits: one page, where more are asked for than memory holds."""
+    refs = torch.zeros(8, dtype=torch.int32)
+    for n in (2 ** 32 + 1, 2 ** 31, -2 ** 32 + 1, 2 ** 63):
+        with pytest.raises(lv.LuvcError) as e:
+            lv.luvc_kv_take(refs, n)
+        assert e.value.status == lv.LUVC_ERR_INVALID_ARG and not refs.any()
